@@ -408,12 +408,143 @@ int cube3d_matmul_blocks(const cube3d_matmul *mm, const void *A_blocks, const vo
  */
 typedef enum cube3d_activation {
     CUBE3D_ACT_RELU = 0,
-    CUBE3D_ACT_GELU = 1
+    CUBE3D_ACT_GELU = 1,
+    CUBE3D_ACT_NONE = 2     /* virtual_cube_linear_fwd_fused only */
 } cube3d_activation;
 
 int cube3d_activation_fwd(int kind, int z_dtype, int h_dtype, int64_t n, const void *z, void *h, void *stream);
 int cube3d_activation_bwd(int kind, int z_dtype, int dh_dtype, int dz_dtype, int64_t n, const void *z, const void *dh,
                           void *dz, void *stream);
+
+/*
+ * A linear layer with what follows it: virtual_cube_linear_fwd with the activation and a residual sum in the same
+ * pass over the result,
+ *     Z = X W + b,   Y = act(Z) + R,
+ * with the sum, the bias, the activation (of the fp32 value, before Z is rounded) and the residual in fp32 and one
+ * rounding each of Y (to shard_dtype) and Z (to z_dtype).  All of X, W, Y, b as for virtual_cube_linear_fwd.
+ *   activation   a cube3d_activation; CUBE3D_ACT_NONE: Y = Z + R
+ *   bias_diag    NULL, or the diagonal storage of b (fp32)
+ *   residual     NULL, or R as a cube of Y shards of residual_dtype (F32 or BF16).  May be Y itself if the two
+ *                types agree: the sum is then formed in place
+ *   z            NULL, or where Z goes: a cube of Y shards of z_dtype (F32 or BF16), for the backward pass
+ * (residual_dtype and z_dtype are ignored where their pointer is NULL.)  Products of few tokens are split along the
+ * contraction and joined in `workspace`: device scratch, 16-byte aligned, of at least
+ * cube3d_epilogue_workspace_bytes(desc, CUBE3D_OP_FWD) bytes (may be NULL when that is 0, else CUBE3D_EWORKSPACE);
+ * contents undefined afterwards.  The order of an element's sum is fixed by the shape: two calls give the same bits.
+ *
+ * virtual_cube_linear_epilogue_bwd: the backward pass of the epilogue,
+ *     dZ = dY * act'(Z),   db = column sums of dZ   (Algorithm 8, as in virtual_cube_bias_bwd),
+ * in one pass over Z and dY.  kind: RELU or GELU (without an activation dZ is dY and db is
+ * virtual_cube_bias_bwd's).  Z, dY, dZ: cubes of Y shards of the three types (F32 or BF16); dZ is rounded once, db is
+ * the sum of the values before that rounding, in fp32 in a fixed order, in diagonal storage (entries off the
+ * diagonal written as zero).  dbias_diag may be NULL: dZ only, no workspace.  Else `workspace` holds at least
+ * cube3d_epilogue_workspace_bytes(desc, CUBE3D_OP_BIAS_BWD) bytes.  dZ may be dY itself if the types agree.  The gradient
+ * of R is dY; dX and dW follow from dZ by virtual_cube_linear_bwd_dx / _dw.
+ */
+typedef struct cube3d_epilogue {
+    int32_t activation;
+    int32_t residual_dtype;
+    int32_t z_dtype;
+    const void *bias_diag;
+    const void *residual;
+    void *z;
+} cube3d_epilogue;
+
+size_t cube3d_epilogue_workspace_bytes(const cube3d_desc *desc, int op);
+int virtual_cube_linear_fwd_fused(const cube3d_desc *desc, const cube3d_epilogue *epilogue, const void *X_shards,
+                                  const void *W_shards, void *Y_shards, void *workspace, size_t workspace_bytes, void *stream);
+int virtual_cube_linear_epilogue_bwd(const cube3d_desc *desc, int kind, int z_dtype, int dy_dtype, int dz_dtype,
+                                     const void *Z_shards, const void *dY_shards, void *dZ_shards, void *dbias_diag,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The norms on either side of a block, with what lies between them (Section 3.2, the residual sums and LayerNorms
+ * around the MLP and attention blocks).  With u the output of a block and x the residual stream it was fed from:
+ *     v = Npost(u)            norm behind the block (NONE: v = u)
+ *     r = x + scale * g * v   the residual stream behind the block; g a gate per column
+ *     n = Npre(r)             norm ahead of the next block
+ * N(t) = (t - mean) * rstd * gamma + beta over the columns of a row, LAYER: rstd = 1 / sqrt(var + eps) with the
+ * variance over all columns; RMS: mean = 0, rstd = 1 / sqrt(mean(t^2) + eps).  All in fp32 (the variance from the
+ * deviations, in a second pass over the row), n from the fp32 value of r; r, n rounded once.
+ *
+ * Placement: `m` names a [rows, cols] matrix stored like activations: row_axis x, col_axis y or z, split by rows, that
+ * is the X shards of a layer whose output direction is col_axis, or the Y shards of one whose input direction it
+ * is; else CUBE3D_EINVAL.  q^2 must divide cols too.  x, r (and dr, dx) are of m->dtype, u, n (du, dn) of
+ * norm->block_dtype: F32 or BF16.  Every vector is fp32 in diagonal storage, as virtual_cube_scatter(desc,
+ * CUBE3D_OPERAND_BIAS) of a layer of N = cols makes it.
+ *   parameters    post_gamma, post_beta belong to Npost, pre_gamma, pre_beta to Npre; NULL: gamma = 1, beta = 0,
+ *                 g = 1.  Ignored where the kind is NONE.
+ *   u             NULL: r = x (nothing written: r must be NULL) and n = Npre(x); post_kind must be NONE.
+ *   r             NULL only if u is
+ *   n             NULL exactly if pre_kind is NONE (one of u and n must be there)
+ *   stats         NULL, or fp32 [rows][4], row by row of the full matrix: mean and rstd of Npost, mean and rstd of Npre
+ *                 (zeros for a kind of NONE, mean 0 for RMS), for the backward pass
+ * r may be x itself.
+ *
+ * virtual_cube_norm_bwd: given dr, the gradient that reaches r other than through n (NULL: none), and dn,
+ *     Dr = dr + Npre'(dn),  dx = Dr,  du = Npost'(scale * g * Dr)
+ * and the gradients of the parameters as column sums over all rows in fp32, in a fixed order (those of Npre from dn, of
+ * Npost and g from Dr in fp32), written to the vectors of `gradients` that are not NULL, in diagonal storage (entries
+ * off the diagonal written as zero).  r is the stored stream behind the block (read if pre_kind is not NONE; the
+ * stream x itself where the forward pass had no u), u the block's output (read if post_kind is not NONE or the gate's gradient is asked for), stats the
+ * forward pass's.  dn is NULL exactly if pre_kind is NONE; dx may be NULL (not written), and so may du; one of dr and dn and
+ * one of the results must be there; without u (NULL) du, post_kind and the gradients of gate and Npost must be absent.  dx may be dr itself.
+ * `workspace`: at least cube3d_norm_workspace_bytes(m, norm) bytes of device scratch, 16-byte aligned, else
+ * CUBE3D_EWORKSPACE.
+ */
+typedef enum cube3d_norm_kind {
+    CUBE3D_NORM_NONE = 0,
+    CUBE3D_NORM_RMS = 1,
+    CUBE3D_NORM_LAYER = 2
+} cube3d_norm_kind;
+
+typedef struct cube3d_norm {
+    int32_t post_kind, pre_kind;    /* cube3d_norm_kind */
+    int32_t block_dtype;            /* type of u, n, du, dn */
+    float post_eps, pre_eps;        /* positive where the kind is not NONE */
+    float scale;                    /* finite */
+} cube3d_norm;
+
+typedef struct cube3d_norm_params {
+    float *post_gamma, *post_beta, *gate, *pre_gamma, *pre_beta;
+} cube3d_norm_params;
+
+size_t cube3d_norm_workspace_bytes(const cube3d_matrix *m, const cube3d_norm *norm);
+int virtual_cube_norm_fwd(const cube3d_matrix *m, const cube3d_norm *norm, const cube3d_norm_params *params,
+                          const void *x, const void *u, void *r, void *n, float *stats, void *stream);
+int virtual_cube_norm_bwd(const cube3d_matrix *m, const cube3d_norm *norm, const cube3d_norm_params *params,
+                          const float *stats, const void *dr, const void *dn, const void *r, const void *u,
+                          void *dx, void *du, const cube3d_norm_params *gradients, void *workspace, size_t workspace_bytes,
+                          void *stream);
+
+/*
+ * The global norm of all gradients of a step, and clipping to a largest norm.
+ * `grads`: host array of `count` device arrays of n elements each, F32 or BF16, 16-byte aligned (n = 0: data may be
+ * NULL), read during the call only.  A cube buffer is one array: the shards of the cube hold every element of
+ * a matrix once, diagonal storage holds zeros off the diagonal.
+ *   cube3d_grad_norm:  *sumsq = sum of g^2 over all elements of all arrays, *norm = scale * sqrt(*sumsq)
+ *       Squares and sums in 64 bits, in an order fixed by the sizes.  sumsq, norm: device memory, aligned to their
+ *       type; norm may be NULL (ranks that share the gradients add their sumsq before they clip).  Every array counts as
+ *       often as it is listed.  workspace: at least cube3d_grad_norm_workspace_bytes(grads, count) bytes, 16-byte
+ *       aligned, else CUBE3D_EWORKSPACE.
+ *   cube3d_grad_clip:  out = f * g  with  f = scale * min(1, max_norm / (scale * sqrt(*sumsq)))
+ *       rounded once to the type of out[k], an array of as many elements as grads[k].  f is formed on the device, in 64
+ *       bits, and rounded to fp32.  A norm that is not finite leaves f = scale: the caller sees it in *norm.
+ *       out[k] may be grads[k] itself (same address and type; nothing is written where f is 1).  Any other overlap
+ *       among the arrays of `out` or of them with those of `grads` is refused (CUBE3D_EINVAL).
+ * scale: positive and finite (the reciprocal of a loss scale, or of a number of accumulated batches); max_norm: positive.
+ */
+typedef struct cube3d_tensor {
+    void *data;
+    int64_t n;
+    int32_t dtype;
+} cube3d_tensor;
+
+size_t cube3d_grad_norm_workspace_bytes(const cube3d_tensor *grads, int count);
+int cube3d_grad_norm(const cube3d_tensor *grads, int count, float scale, double *sumsq, float *norm, void *workspace,
+                     size_t workspace_bytes, void *stream);
+int cube3d_grad_clip(const cube3d_tensor *grads, const cube3d_tensor *out, int count, float scale, float max_norm,
+                     const double *sumsq, void *stream);
 
 /* One-time set-up of every kernel variant on the calling thread's current device (optional:
  * a variant is otherwise set up on its first use).  Enqueues nothing.  CUBE3D_ELAUNCH when

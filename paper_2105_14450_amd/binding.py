@@ -19,7 +19,8 @@ OPERAND_X, OPERAND_W, OPERAND_DY, OPERAND_Y, OPERAND_DX, OPERAND_DW, OPERAND_BIA
 OP_FWD, OP_BWD_DX, OP_BWD_DW, OP_BIAS_BWD = 0, 1, 2, 3
 SPLIT_ROWS, SPLIT_COLS = 0, 1
 FORM_AB, FORM_ABT, FORM_ATB = 0, 1, 2
-ACT_RELU, ACT_GELU = 0, 1
+ACT_RELU, ACT_GELU, ACT_NONE = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 ALL_RANKS = (-1, -1, -1)
 
 DTYPE_CODES = {"f32": F32, "bf16": BF16, "fp8_e4m3": FP8_E4M3}
@@ -64,6 +65,66 @@ def make_matrix(q, rows, cols, row_axis, col_axis, split, dtype) -> Matrix:
 
 def make_matmul(q, form, m, n, k, in_dtype=BF16, out_dtype=F32, scale_a=1.0, scale_b=1.0) -> Matmul:
     return Matmul(q, form, m, n, k, in_dtype, out_dtype, scale_a, scale_b)
+
+
+class Epilogue(ctypes.Structure):
+    """Mirror of ``cube3d_epilogue``; keeps the tensors it points to alive."""
+    _fields_ = [("activation", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("z_dtype", ctypes.c_int32),
+                ("bias_diag", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("z", ctypes.c_void_p)]
+
+
+class Norm(ctypes.Structure):
+    """Mirror of ``cube3d_norm``."""
+    _fields_ = [("post_kind", ctypes.c_int32), ("pre_kind", ctypes.c_int32), ("block_dtype", ctypes.c_int32),
+                ("post_eps", ctypes.c_float), ("pre_eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class NormParams(ctypes.Structure):
+    """Mirror of ``cube3d_norm_params``; keeps the tensors it points to alive."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("post_gamma", "post_beta", "gate", "pre_gamma", "pre_beta")]
+
+
+class Tensor(ctypes.Structure):
+    """Mirror of ``cube3d_tensor``."""
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32)]
+
+
+def make_epilogue(activation=ACT_NONE, bias=None, residual=None, residual_dtype=BF16, z=None, z_dtype=BF16) -> Epilogue:
+    e = Epilogue(activation, residual_dtype, z_dtype, _ptr(bias), _ptr(residual), _ptr(z))
+    e.tensors = (bias, residual, z)
+    return e
+
+
+def make_norm(pre=NORM_NONE, post=NORM_NONE, block_dtype=BF16, pre_eps=1e-5, post_eps=1e-5, scale=1.0) -> Norm:
+    return Norm(post, pre, block_dtype, post_eps, pre_eps, scale)
+
+
+def make_norm_params(post_gamma=None, post_beta=None, gate=None, pre_gamma=None, pre_beta=None) -> NormParams:
+    tensors = (post_gamma, post_beta, gate, pre_gamma, pre_beta)
+    p = NormParams(*[_ptr(t) for t in tensors])
+    p.tensors = tensors
+    return p
+
+
+class TensorList:
+    """Device arrays as the gradient calls take them; made once for tensors that stay where they are."""
+
+    def __init__(self, tensors, dtypes):
+        self.tensors, self.count = tuple(tensors), len(tensors)
+        self.array = (Tensor * max(1, self.count))(*[Tensor(_ptr(t) if t.numel() else None, t.numel(), code)
+                                                    for t, code in zip(tensors, dtypes)])
+
+
+def make_tensor_list(tensors, dtypes=None) -> TensorList:
+    """dtypes: a dtype code per tensor (for tensors that only hold bytes), else torch's float32 and bfloat16 name theirs."""
+    import torch
+    tensors = list(tensors)
+    if dtypes is None:
+        dtypes = [{torch.float32: F32, torch.bfloat16: BF16}[t.dtype] for t in tensors]
+    dtypes = list(dtypes)
+    if len(dtypes) != len(tensors):
+        raise ValueError("one dtype per tensor")
+    return TensorList(tensors, dtypes)
 
 
 class Cube3DError(RuntimeError):
@@ -132,6 +193,26 @@ def load():
     lib.cube3d_activation_fwd.restype = ci
     lib.cube3d_activation_bwd.argtypes = [ci, ci, ci, ci, ctypes.c_int64, vp, vp, vp, vp]
     lib.cube3d_activation_bwd.restype = ci
+    ep, np_, pp_, tp = ctypes.POINTER(Epilogue), ctypes.POINTER(Norm), ctypes.POINTER(NormParams), ctypes.POINTER(Tensor)
+    cf = ctypes.c_float
+    lib.cube3d_epilogue_workspace_bytes.argtypes = [dp, ci]
+    lib.cube3d_epilogue_workspace_bytes.restype = sz
+    lib.virtual_cube_linear_fwd_fused.argtypes = [dp, ep, vp, vp, vp, vp, sz, vp]
+    lib.virtual_cube_linear_fwd_fused.restype = ci
+    lib.virtual_cube_linear_epilogue_bwd.argtypes = [dp, ci, ci, ci, ci, vp, vp, vp, vp, vp, sz, vp]
+    lib.virtual_cube_linear_epilogue_bwd.restype = ci
+    lib.cube3d_norm_workspace_bytes.argtypes = [mp, np_]
+    lib.cube3d_norm_workspace_bytes.restype = sz
+    lib.virtual_cube_norm_fwd.argtypes = [mp, np_, pp_, vp, vp, vp, vp, vp, vp]
+    lib.virtual_cube_norm_fwd.restype = ci
+    lib.virtual_cube_norm_bwd.argtypes = [mp, np_, pp_, vp, vp, vp, vp, vp, vp, vp, pp_, vp, sz, vp]
+    lib.virtual_cube_norm_bwd.restype = ci
+    lib.cube3d_grad_norm_workspace_bytes.argtypes = [tp, ci]
+    lib.cube3d_grad_norm_workspace_bytes.restype = sz
+    lib.cube3d_grad_norm.argtypes = [tp, ci, cf, vp, vp, vp, sz, vp]
+    lib.cube3d_grad_norm.restype = ci
+    lib.cube3d_grad_clip.argtypes = [tp, tp, ci, cf, cf, vp, vp]
+    lib.cube3d_grad_clip.restype = ci
     lib.cube3d_status_string.argtypes = [ci]
     lib.cube3d_status_string.restype = ctypes.c_char_p
     lib.cube3d_version.restype = ci
@@ -150,7 +231,10 @@ EXPORTS = ("cube3d_linear_fwd", "cube3d_linear_bwd_dx", "cube3d_linear_bwd_dw", 
            "virtual_cube_linear_bwd_dw", "virtual_cube_matrix_scatter", "virtual_cube_matrix_assemble",
            "virtual_cube_matrix_gather", "virtual_cube_matrix_reduce_scatter", "cube3d_matmul_workspace_bytes",
            "cube3d_matmul_blocks", "virtual_cube_matmul", "cube3d_activation_fwd", "cube3d_activation_bwd", "cube3d_status_string",
-           "cube3d_version", "cube3d_init", "cube3d_linear_bwd_dw_noalloc")
+           "cube3d_version", "cube3d_init", "cube3d_linear_bwd_dw_noalloc", "cube3d_epilogue_workspace_bytes",
+           "virtual_cube_linear_fwd_fused", "virtual_cube_linear_epilogue_bwd", "cube3d_norm_workspace_bytes",
+           "virtual_cube_norm_fwd", "virtual_cube_norm_bwd", "cube3d_grad_norm_workspace_bytes", "cube3d_grad_norm",
+           "cube3d_grad_clip")
 
 
 def status_string(status: int) -> str:
@@ -330,6 +414,64 @@ def virtual_cube_matmul(form, A, B, C, A_pieces, B_pieces, C_pieces, scale_a=1.0
                                       _ptr(A_pieces), _ptr(B_pieces), _ptr(C_pieces), _stream(stream)),
            "virtual_cube_matmul")
     return C_pieces
+
+
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def cube3d_epilogue_workspace_bytes(desc: Desc, op: int) -> int:
+    return int(load().cube3d_epilogue_workspace_bytes(ctypes.byref(desc), op))
+
+
+def virtual_cube_linear_fwd_fused(desc, epilogue, X_shards, W_shards, Y_shards, workspace=None, stream=None):
+    _check(load().virtual_cube_linear_fwd_fused(ctypes.byref(desc), ctypes.byref(epilogue), _ptr(X_shards), _ptr(W_shards),
+                                                _ptr(Y_shards), _ptr(workspace), _bytes(workspace), _stream(stream)),
+           "virtual_cube_linear_fwd_fused")
+    return Y_shards
+
+
+def virtual_cube_linear_epilogue_bwd(desc, kind, z_dtype, dy_dtype, dz_dtype, Z_shards, dY_shards, dZ_shards, dbias_diag=None,
+                                     workspace=None, stream=None):
+    _check(load().virtual_cube_linear_epilogue_bwd(ctypes.byref(desc), kind, z_dtype, dy_dtype, dz_dtype, _ptr(Z_shards),
+                                                   _ptr(dY_shards), _ptr(dZ_shards), _ptr(dbias_diag), _ptr(workspace),
+                                                   _bytes(workspace), _stream(stream)), "virtual_cube_linear_epilogue_bwd")
+    return dZ_shards
+
+
+def cube3d_norm_workspace_bytes(m: Matrix, norm: Norm) -> int:
+    return int(load().cube3d_norm_workspace_bytes(ctypes.byref(m), ctypes.byref(norm)))
+
+
+def virtual_cube_norm_fwd(m, norm, params, x, u, r, n, stats=None, stream=None):
+    _check(load().virtual_cube_norm_fwd(ctypes.byref(m), ctypes.byref(norm), ctypes.byref(params), _ptr(x), _ptr(u), _ptr(r),
+                                        _ptr(n), _ptr(stats), _stream(stream)), "virtual_cube_norm_fwd")
+    return r, n
+
+
+def virtual_cube_norm_bwd(m, norm, params, stats, dr, dn, r, u, dx, du, gradients, workspace, stream=None):
+    _check(load().virtual_cube_norm_bwd(ctypes.byref(m), ctypes.byref(norm), ctypes.byref(params), _ptr(stats), _ptr(dr), _ptr(dn),
+                                        _ptr(r), _ptr(u), _ptr(dx), _ptr(du), ctypes.byref(gradients), _ptr(workspace),
+                                        _bytes(workspace), _stream(stream)), "virtual_cube_norm_bwd")
+    return dx, du
+
+
+def cube3d_grad_norm_workspace_bytes(grads: TensorList) -> int:
+    return int(load().cube3d_grad_norm_workspace_bytes(grads.array, grads.count))
+
+
+def cube3d_grad_norm(grads, sumsq, norm=None, workspace=None, scale=1.0, stream=None):
+    _check(load().cube3d_grad_norm(grads.array, grads.count, scale, _ptr(sumsq), _ptr(norm), _ptr(workspace), _bytes(workspace),
+                                   _stream(stream)), "cube3d_grad_norm")
+    return norm
+
+
+def cube3d_grad_clip(grads, out, sumsq, max_norm, scale=1.0, stream=None):
+    if out.count != grads.count:
+        raise ValueError("as many results as gradients")
+    _check(load().cube3d_grad_clip(grads.array, out.array, grads.count, scale, max_norm, _ptr(sumsq), _stream(stream)),
+           "cube3d_grad_clip")
+    return out
 
 
 def cube3d_init() -> None:

@@ -107,6 +107,7 @@ size_t workspace_for(const GemmArgs &a)
 // The first kernel family that takes the product: tile-aligned sizes, then any size, then element by element.
 int run_gemm(const GemmArgs &a)
 {
+    if (a.epilogue) return gemm_generic(a);
     const FastPlan plan = gemm_fast_plan(a);
     const size_t need = gemm_fast_workspace(a, plan);
     if (need > 0 && (!a.workspace || a.workspace_bytes < need)) return CUBE3D_EWORKSPACE;
@@ -156,7 +157,8 @@ ShardMaps shard_maps(const CubeGeom &g)
 }
 
 // One product over the whole cube with the shards read and written in place.
-int run_cube_product(const cube3d_desc *d, int op, const void *A, const void *B, const void *bias, void *C, void *stream)
+int run_cube_product(const cube3d_desc *d, int op, const void *A, const void *B, const void *bias, void *C, void *stream,
+                     const Epilogue *epilogue = nullptr)
 {
     CubeGeom g;
     int rc = check_desc(d, &g);
@@ -197,6 +199,7 @@ int run_cube_product(const cube3d_desc *d, int op, const void *A, const void *B,
     }
     if (mp.bias == nullptr) mp.bias_n = sm.bn;
     a.maps = &mp;
+    a.epilogue = epilogue;
     return run_gemm(a);
 }
 
@@ -579,6 +582,77 @@ int cube3d_matmul_blocks(const cube3d_matmul *mm, const void *A_blocks, const vo
 
 }  // extern "C"
 
+// ---- the operators around the linear layers: epilogue, norms, gradient clipping ---------------------------
+namespace {
+
+bool f32_or_bf16(int dtype) { return dtype == CUBE3D_F32 || dtype == CUBE3D_BF16; }
+
+bool misaligned(const cube3d_norm_params &p)
+{
+    for (const float *v : {p.post_gamma, p.post_beta, p.gate, p.pre_gamma, p.pre_beta})
+        if (misaligned(v)) return true;
+    return false;
+}
+
+// Placement, sizes, types and kinds of a norm call.
+int check_norm(const cube3d_matrix *m, const cube3d_norm *norm, NormArgs *out)
+{
+    CubeGeom g;
+    int rc = check_matrix(m, &g);
+    if (rc != CUBE3D_OK) return rc;
+    if (m->row_axis != CUBE3D_AXIS_X || m->split != CUBE3D_SPLIT_ROWS) return CUBE3D_EINVAL;
+    if (m->cols % ((int64_t)m->q * m->q)) return CUBE3D_ESHAPE;
+    if (m->rows >= (1ll << 31) || m->cols >= (1ll << 31)) return CUBE3D_ESHAPE;
+    if (!norm) return CUBE3D_EINVAL;
+    if (!f32_or_bf16(m->dtype) || !f32_or_bf16(norm->block_dtype)) return CUBE3D_EDTYPE;
+    for (int kind : {norm->post_kind, norm->pre_kind})
+        if (kind != CUBE3D_NORM_NONE && kind != CUBE3D_NORM_RMS && kind != CUBE3D_NORM_LAYER) return CUBE3D_EINVAL;
+    if (norm->post_kind != CUBE3D_NORM_NONE && (!(norm->post_eps > 0.f) || norm->post_eps > 3.0e38f)) return CUBE3D_EINVAL;
+    if (norm->pre_kind != CUBE3D_NORM_NONE && (!(norm->pre_eps > 0.f) || norm->pre_eps > 3.0e38f)) return CUBE3D_EINVAL;
+    if (!(norm->scale >= -3.0e38f && norm->scale <= 3.0e38f)) return CUBE3D_EINVAL;
+    NormArgs a{};
+    a.row = place_row_map(g);
+    a.col = place_col_map(g);
+    // vector element c Cb + p Cs + x on the processor (p, c, c)
+    const int64_t Cs = g.pCb / g.q;
+    a.vec = AxisMap{(int32_t)g.pCb, (int32_t)Cs, (g.q + 1) * Cs, (int64_t)g.q * g.q * Cs, 1};
+    for (AxisMap *x : {&a.row, &a.col, &a.vec}) prepare_axis_map(*x);
+    a.rows = m->rows;
+    a.cols = (int)m->cols;
+    a.q = m->q;
+    a.post_kind = norm->post_kind;
+    a.pre_kind = norm->pre_kind;
+    a.stream_f32 = m->dtype == CUBE3D_F32;
+    a.block_f32 = norm->block_dtype == CUBE3D_F32;
+    a.post_eps = norm->post_eps;
+    a.pre_eps = norm->pre_eps;
+    a.scale = norm->scale;
+    *out = a;
+    return CUBE3D_OK;
+}
+
+// The parameters that a call uses.
+cube3d_norm_params used_params(const cube3d_norm &norm, cube3d_norm_params p, bool block)
+{
+    if (norm.post_kind == CUBE3D_NORM_NONE) p.post_gamma = p.post_beta = nullptr;
+    if (norm.pre_kind == CUBE3D_NORM_NONE) p.pre_gamma = p.pre_beta = nullptr;
+    if (!block) p.gate = nullptr;
+    return p;
+}
+
+int check_tensors(const cube3d_tensor *t, int count)
+{
+    if (count < 0 || (count > 0 && !t)) return CUBE3D_EINVAL;
+    for (int k = 0; k < count; ++k) {
+        if (t[k].n < 0 || t[k].n >= (1ll << 48)) return CUBE3D_ESHAPE;
+        if (!f32_or_bf16(t[k].dtype)) return CUBE3D_EDTYPE;
+        if (t[k].n > 0 && (!t[k].data || misaligned(t[k].data))) return CUBE3D_EINVAL;
+    }
+    return CUBE3D_OK;
+}
+
+}  // namespace
+
 extern "C" {
 
 int cube3d_activation_fwd(int kind, int z_dtype, int h_dtype, int64_t n, const void *z, void *h, void *stream)
@@ -602,6 +676,143 @@ int cube3d_activation_bwd(int kind, int z_dtype, int dh_dtype, int dz_dtype, int
     if (!z || !dh || !dz || misaligned(z) || misaligned(dh) || misaligned(dz)) return CUBE3D_EINVAL;
     if (n == 0) return CUBE3D_OK;
     return activation_bwd(kind, z_dtype, dh_dtype, dz_dtype, n, z, dh, dz, static_cast<hipStream_t>(stream));
+}
+
+size_t cube3d_epilogue_workspace_bytes(const cube3d_desc *desc, int op)
+{
+    CubeGeom g;
+    if (check_desc(desc, &g) != CUBE3D_OK) return 0;
+    if (op == CUBE3D_OP_BIAS_BWD) return epilogue_bwd_workspace(g);
+    return 0;
+}
+
+int virtual_cube_linear_fwd_fused(const cube3d_desc *desc, const cube3d_epilogue *epilogue, const void *X_shards,
+                                  const void *W_shards, void *Y_shards, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int rc = check_desc(desc, nullptr);
+    if (rc != CUBE3D_OK) return rc;
+    if (!epilogue) return CUBE3D_EINVAL;
+    if (epilogue->activation != CUBE3D_ACT_NONE && epilogue->activation != CUBE3D_ACT_RELU && epilogue->activation != CUBE3D_ACT_GELU)
+        return CUBE3D_EINVAL;
+    if (epilogue->residual && !f32_or_bf16(epilogue->residual_dtype)) return CUBE3D_EDTYPE;
+    if (epilogue->z && !f32_or_bf16(epilogue->z_dtype)) return CUBE3D_EDTYPE;
+    if (misaligned(epilogue->residual) || misaligned(epilogue->z) || misaligned(workspace)) return CUBE3D_EINVAL;
+    // in place only element by element: Z may not be Y, nor either of them a residual of another type
+    if (epilogue->z && (epilogue->z == Y_shards || epilogue->z == epilogue->residual)) return CUBE3D_EINVAL;
+    if (epilogue->residual == Y_shards && Y_shards && epilogue->residual_dtype != desc->shard_dtype) return CUBE3D_EINVAL;
+    const Epilogue e{epilogue->activation, epilogue->residual && epilogue->residual_dtype == CUBE3D_F32,
+                     epilogue->z && epilogue->z_dtype == CUBE3D_F32, epilogue->residual, epilogue->z};
+    (void)workspace_bytes;
+    return run_cube_product(desc, CUBE3D_OP_FWD, X_shards, W_shards, epilogue->bias_diag, Y_shards, stream, &e);
+}
+
+int virtual_cube_linear_epilogue_bwd(const cube3d_desc *desc, int kind, int z_dtype, int dy_dtype, int dz_dtype,
+                                     const void *Z_shards, const void *dY_shards, void *dZ_shards, void *dbias_diag,
+                                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    CubeGeom g;
+    int rc = check_desc(desc, &g);
+    if (rc != CUBE3D_OK) return rc;
+    if (kind != CUBE3D_ACT_RELU && kind != CUBE3D_ACT_GELU) return CUBE3D_EINVAL;
+    if (!f32_or_bf16(z_dtype) || !f32_or_bf16(dy_dtype) || !f32_or_bf16(dz_dtype)) return CUBE3D_EDTYPE;
+    if (!Z_shards || !dY_shards || !dZ_shards) return CUBE3D_EINVAL;
+    if (misaligned(Z_shards) || misaligned(dY_shards) || misaligned(dZ_shards) || misaligned(dbias_diag) || misaligned(workspace))
+        return CUBE3D_EINVAL;
+    if (dZ_shards == Z_shards || (dZ_shards == dY_shards && dz_dtype != dy_dtype)) return CUBE3D_EINVAL;
+    if (dbias_diag && (!workspace || workspace_bytes < epilogue_bwd_workspace(g))) return CUBE3D_EWORKSPACE;
+    return epilogue_bwd(g, kind, z_dtype, dy_dtype, dz_dtype, Z_shards, dY_shards, dZ_shards, static_cast<float *>(dbias_diag),
+                        static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
+}
+
+size_t cube3d_norm_workspace_bytes(const cube3d_matrix *m, const cube3d_norm *norm)
+{
+    NormArgs a;
+    return check_norm(m, norm, &a) == CUBE3D_OK ? norm_bwd_workspace(a) : 0;
+}
+
+int virtual_cube_norm_fwd(const cube3d_matrix *m, const cube3d_norm *norm, const cube3d_norm_params *params,
+                          const void *x, const void *u, void *r, void *n, float *stats, void *stream)
+{
+    NormArgs a;
+    int rc = check_norm(m, norm, &a);
+    if (rc != CUBE3D_OK) return rc;
+    if (!params || misaligned(*params)) return CUBE3D_EINVAL;
+    if (!x || (!u && !n)) return CUBE3D_EINVAL;
+    if ((u == nullptr) != (r == nullptr) || (n == nullptr) != (norm->pre_kind == CUBE3D_NORM_NONE)) return CUBE3D_EINVAL;
+    if (!u && norm->post_kind != CUBE3D_NORM_NONE) return CUBE3D_EINVAL;
+    for (const void *p : {x, u, (const void *)r, (const void *)n, (const void *)stats})
+        if (misaligned(p)) return CUBE3D_EINVAL;
+    if (n && (n == x || n == u || n == r)) return CUBE3D_EINVAL;      // n is written while x and u are still read
+    if (r && r == u) return CUBE3D_EINVAL;
+    a.p = used_params(*norm, *params, u != nullptr);
+    a.x = x; a.u = u;
+    a.r_out = r; a.n_out = n; a.stats_out = stats;
+    return norm_fwd(a, static_cast<hipStream_t>(stream));
+}
+
+int virtual_cube_norm_bwd(const cube3d_matrix *m, const cube3d_norm *norm, const cube3d_norm_params *params,
+                          const float *stats, const void *dr, const void *dn, const void *r, const void *u,
+                          void *dx, void *du, const cube3d_norm_params *gradients, void *workspace, size_t workspace_bytes,
+                          void *stream)
+{
+    NormArgs a;
+    int rc = check_norm(m, norm, &a);
+    if (rc != CUBE3D_OK) return rc;
+    if (!params || !gradients || misaligned(*params) || misaligned(*gradients)) return CUBE3D_EINVAL;
+    const bool pre = norm->pre_kind != CUBE3D_NORM_NONE, post = norm->post_kind != CUBE3D_NORM_NONE;
+    const cube3d_norm_params &d = *gradients;
+    if ((dn == nullptr) == pre || (!dr && !dn) || (pre && !r)) return CUBE3D_EINVAL;
+    if ((pre || post) && !stats) return CUBE3D_EINVAL;
+    if (!u && (du || post || d.gate)) return CUBE3D_EINVAL;
+    if (!post && (d.post_gamma || d.post_beta)) return CUBE3D_EINVAL;
+    if (!pre && (d.pre_gamma || d.pre_beta)) return CUBE3D_EINVAL;
+    const bool sums = d.post_gamma || d.post_beta || d.gate || d.pre_gamma || d.pre_beta;
+    if (!dx && !du && !sums) return CUBE3D_EINVAL;
+    for (const void *p : {(const void *)stats, dr, dn, r, u, (const void *)dx, (const void *)du, (const void *)workspace})
+        if (misaligned(p)) return CUBE3D_EINVAL;
+    for (const void *in : {dn, r, u})
+        if (in && (in == dx || in == du)) return CUBE3D_EINVAL;
+    if (du && (du == dr || du == dx)) return CUBE3D_EINVAL;
+    if (!workspace || workspace_bytes < norm_bwd_workspace(a)) return CUBE3D_EWORKSPACE;
+    a.p = used_params(*norm, *params, u != nullptr);
+    a.x = r; a.u = u;
+    a.stats = stats; a.dr = dr; a.dn = dn; a.dx = dx; a.du = du;
+    a.read_u = post || d.gate;
+    a.sums = sums;
+    return norm_bwd(a, d, workspace, static_cast<hipStream_t>(stream));
+}
+
+size_t cube3d_grad_norm_workspace_bytes(const cube3d_tensor *grads, int count)
+{
+    return check_tensors(grads, count) == CUBE3D_OK ? (size_t)grad_norm_partials(grads, count) * sizeof(double) : 0;
+}
+
+int cube3d_grad_norm(const cube3d_tensor *grads, int count, float scale, double *sumsq, float *norm, void *workspace,
+                     size_t workspace_bytes, void *stream)
+{
+    const int rc = check_tensors(grads, count);
+    if (rc != CUBE3D_OK) return rc;
+    if (!(scale > 0.f) || scale > 3.4028235e38f) return CUBE3D_EINVAL;
+    if (!sumsq || reinterpret_cast<uintptr_t>(sumsq) % 8 || reinterpret_cast<uintptr_t>(norm) % 4 || misaligned(workspace))
+        return CUBE3D_EINVAL;
+    const size_t need = (size_t)grad_norm_partials(grads, count) * sizeof(double);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return CUBE3D_EWORKSPACE;
+    return grad_norm(grads, count, scale, sumsq, norm, static_cast<double *>(workspace), static_cast<hipStream_t>(stream));
+}
+
+int cube3d_grad_clip(const cube3d_tensor *grads, const cube3d_tensor *out, int count, float scale, float max_norm,
+                     const double *sumsq, void *stream)
+{
+    int rc = check_tensors(grads, count);
+    if (rc == CUBE3D_OK) rc = check_tensors(out, count);
+    if (rc != CUBE3D_OK) return rc;
+    if (!(scale > 0.f) || scale > 3.4028235e38f || !(max_norm > 0.f)) return CUBE3D_EINVAL;
+    if (!sumsq || reinterpret_cast<uintptr_t>(sumsq) % 8) return CUBE3D_EINVAL;
+    for (int k = 0; k < count; ++k)
+        if (grads[k].n != out[k].n) return CUBE3D_ESHAPE;
+    rc = check_clip_overlap(grads, out, count);
+    if (rc != CUBE3D_OK) return rc;
+    return grad_clip(grads, out, count, scale, max_norm, sumsq, static_cast<hipStream_t>(stream));
 }
 
 int cube3d_init(void)

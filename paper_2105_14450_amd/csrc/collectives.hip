@@ -690,6 +690,13 @@ int cube_bias_move(const CubeGeom &g, int mode, const float *src, float *dst, hi
     return launch_status();
 }
 
+int cube_bias_finish(const CubeGeom &g, int NRG, float scale, const float *part, float *dbias_diag, hipStream_t stream)
+{
+    dim3 grid((unsigned)(g.q * g.q * g.q), (unsigned)((g.Ns + 63) / 64), 1);
+    hipLaunchKernelGGL(cube_bias_bwd_finish_kernel, grid, dim3(64 * FIN_WAVES), 0, stream, g, NRG, scale, part, dbias_diag);
+    return launch_status();
+}
+
 size_t cube_bias_bwd_workspace(const CubeGeom &g, int dy_dtype)
 {
     const int es = dy_dtype == CUBE3D_F32 ? 4 : dy_dtype == CUBE3D_BF16 ? 2 : 1;
@@ -713,10 +720,7 @@ int cube_bias_bwd(const CubeGeom &g, int dy_dtype, float scale_dy, const void *d
     case CUBE3D_BF16: launch_bias_bwd_rows<unsigned short>(g, RG, NRG, dy_shards, part, stream); break;
     default: launch_bias_bwd_rows<unsigned char>(g, RG, NRG, dy_shards, part, stream); break;
     }
-    dim3 grid2((unsigned)(g.q * g.q * g.q), (unsigned)((g.Ns + 63) / 64), 1);
-    hipLaunchKernelGGL(cube_bias_bwd_finish_kernel, grid2, dim3(64 * FIN_WAVES), 0, stream, g, NRG,
-                       dy_dtype == CUBE3D_FP8_E4M3 ? scale_dy : 1.f, part, dbias_diag);
-    return launch_status();
+    return cube_bias_finish(g, NRG, dy_dtype == CUBE3D_FP8_E4M3 ? scale_dy : 1.f, part, dbias_diag, stream);
 }
 
 }  // namespace cube3d

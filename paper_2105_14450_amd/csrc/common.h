@@ -87,6 +87,15 @@ struct GemmMaps {
     const float *bias;
 };
 
+// What follows a product of the forward layout with maps:  z = alpha acc + bias;  y = act(z) + residual.  residual and z are
+// addressed like the output (in elements of their own types).
+struct Epilogue {
+    int act;                            // cube3d_activation
+    int residual_f32, z_f32;
+    const void *residual;               // or nullptr
+    void *z;                            // or nullptr
+};
+
 // One (possibly batched) product  C[Mo,No] = alpha * opA * opB  with fp32 accumulation.
 //   a_kmajor: A is stored [Mo, Kc] (contraction index contiguous), else [Kc, Mo]
 //   b_kmajor: B is stored [No, Kc] (contraction index contiguous), else [Kc, No]
@@ -111,6 +120,8 @@ struct GemmArgs {
     // nullptr: plain row-major operands (lda / ldb / ldc).  Otherwise the operands and the output
     // are addressed through these maps (batch must be 1; leading dimensions and strides unused).
     const GemmMaps *maps;
+    // nullptr, or what follows the product (forward layout with maps, batch 1)
+    const Epilogue *epilogue;
 };
 
 // Any shape, any supported dtype; bounds-checked.  Returns a cube3d_status.
@@ -177,11 +188,48 @@ int cube_bias_move(const CubeGeom &g, int mode, const float *src, float *dst, hi
 size_t cube_bias_bwd_workspace(const CubeGeom &g, int dy_dtype);
 int cube_bias_bwd(const CubeGeom &g, int dy_dtype, float scale_dy, const void *dy_shards, float *dbias_diag,
                   void *workspace, size_t workspace_bytes, hipStream_t stream);
+// Its second stage: partial column sums [q^3][NRG][Nb] of the processors' row groups, added in ascending order onto the diagonal.
+int cube_bias_finish(const CubeGeom &g, int NRG, float scale, const float *part, float *dbias_diag, hipStream_t stream);
+
+// Backward pass of a linear layer's epilogue: dz = dy act'(z) on cubes of Y shards, with the column sums (dbias may be nullptr).
+size_t epilogue_bwd_workspace(const CubeGeom &g);
+int epilogue_bwd(const CubeGeom &g, int kind, int z_dtype, int dy_dtype, int dz_dtype, const void *z, const void *dy, void *dz,
+                 float *dbias_diag, float *workspace, hipStream_t stream);
 
 // Element-wise activation over n elements (dtypes F32 or BF16 already checked by the caller).
 int activation_fwd(int kind, int z_dtype, int h_dtype, int64_t n, const void *z, void *h, hipStream_t stream);
 int activation_bwd(int kind, int z_dtype, int g_dtype, int dz_dtype, int64_t n, const void *z, const void *dh, void *dz,
                    hipStream_t stream);
+
+// The norms around a block, forward and backward, on a matrix stored like activations: element (row, column) at row(row) +
+// col(column), element `column` of a vector in diagonal storage at vec(column) (all three prepared).
+struct NormArgs {
+    AxisMap row, col, vec;
+    int64_t rows;
+    int cols, q;
+    int post_kind, pre_kind;
+    bool stream_f32, block_f32;
+    float post_eps, pre_eps, scale;
+    cube3d_norm_params p;
+    const void *x, *u;              // backward: x is the stored stream behind the block
+    void *r_out, *n_out;
+    float *stats_out;
+    const float *stats;             // backward
+    const void *dr, *dn;
+    void *dx, *du;
+    bool read_u, sums;              // u is read; any column sum is wanted
+};
+int norm_fwd(const NormArgs &a, hipStream_t stream);
+size_t norm_bwd_workspace(const NormArgs &a);      // of rows, cols alone
+int norm_bwd(const NormArgs &a, const cube3d_norm_params &gradients, void *workspace, hipStream_t stream);
+
+// Gradient norm and clipping over lists of arrays that the caller has checked.  Partial sums (doubles) of grad_norm:
+int64_t grad_norm_partials(const cube3d_tensor *grads, int count);
+int grad_norm(const cube3d_tensor *grads, int count, float scale, double *sumsq, float *norm, double *partials, hipStream_t stream);
+int grad_clip(const cube3d_tensor *grads, const cube3d_tensor *out, int count, float scale, float max_norm, const double *sumsq,
+              hipStream_t stream);
+// CUBE3D_EINVAL where a result overlaps a gradient (other than itself, in place) or another result.
+int check_clip_overlap(const cube3d_tensor *grads, const cube3d_tensor *out, int count);
 
 inline int launch_status()
 {

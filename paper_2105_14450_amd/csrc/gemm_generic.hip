@@ -6,7 +6,7 @@
 // (4 wavefronts) makes a 64x64 output tile; each wavefront owns one 32x32 MFMA accumulator.
 //
 // Implements the local products of Algorithm 1 step 3 and Algorithm 2 lines 1-2.
-#include "common.h"
+#include "activation.h"
 
 namespace cube3d {
 namespace {
@@ -60,12 +60,13 @@ template <> __device__ __forceinline__ void store_out<unsigned short>(unsigned s
 }
 
 // MAPPED: every element address goes through the index maps (operands and output are cubes of
-// shards, Section 3.1.1) and the optional bias is added; the leading dimensions are unused.
-template <typename TIn, typename TOut, bool AK, bool BK, bool MAPPED>
+// shards, Section 3.1.1) and the optional bias is added; the leading dimensions are unused.  EPI: and what follows the
+// product is applied.
+template <typename TIn, typename TOut, bool AK, bool BK, bool MAPPED, bool EPI = false>
 __global__ __launch_bounds__(256) void gemm_generic_kernel(const TIn *__restrict__ A, const TIn *__restrict__ B,
                                                            TOut *__restrict__ C, int64_t Mo, int64_t No, int64_t Kc,
                                                            int64_t lda, int64_t ldb, int64_t ldc, int64_t sA,
-                                                           int64_t sB, int64_t sC, float alpha, GemmMaps maps)
+                                                           int64_t sB, int64_t sC, float alpha, GemmMaps maps, Epilogue epi)
 {
     // address of operand element (mn, k): plain leading dimension, or the two index maps
     auto a_at = [&](int64_t gm, int64_t gk) -> int64_t {
@@ -141,6 +142,10 @@ __global__ __launch_bounds__(256) void gemm_generic_kernel(const TIn *__restrict
             const int64_t row = m0 + wm + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3);
             if (row < Mo) {
                 const int64_t row_off = MAPPED ? axis_offset(maps.c_m, row) : row * ldc;
+                if (EPI) {
+                    store_out<TOut>(C + row_off + col_off, epilogue_element(epi, acc[v] * alpha + bias, row_off + col_off));
+                    continue;
+                }
                 store_out<TOut>(C + row_off + col_off, MAPPED ? acc[v] * alpha + bias : acc[v] * alpha);
             }
         }
@@ -156,9 +161,16 @@ int launch_layout(const GemmArgs &g)
     const TIn *B = static_cast<const TIn *>(g.B);
     TOut *C = static_cast<TOut *>(g.C);
     const GemmMaps maps = g.maps ? *g.maps : GemmMaps{};
+    const Epilogue epi = g.epilogue ? *g.epilogue : Epilogue{};
+    if (g.epilogue) {
+        if (!g.maps || g.batch != 1 || !g.a_kmajor || g.b_kmajor) return CUBE3D_EINVAL;
+        hipLaunchKernelGGL((gemm_generic_kernel<TIn, TOut, true, false, true, true>), grid, block, 0, g.stream, A, B, C, g.Mo, g.No, g.Kc,
+                           g.lda, g.ldb, g.ldc, g.strideA, g.strideB, g.strideC, g.alpha, maps, epi);
+        return launch_status();
+    }
 #define CUBE3D_LAUNCH(AKV, BKV, MP)                                                                               \
     hipLaunchKernelGGL((gemm_generic_kernel<TIn, TOut, AKV, BKV, MP>), grid, block, 0, g.stream, A, B, C, g.Mo, \
-                       g.No, g.Kc, g.lda, g.ldb, g.ldc, g.strideA, g.strideB, g.strideC, g.alpha, maps)
+                       g.No, g.Kc, g.lda, g.ldb, g.ldc, g.strideA, g.strideB, g.strideC, g.alpha, maps, epi)
     if (g.maps) {
         if (g.batch != 1) return CUBE3D_EINVAL;
         if (g.a_kmajor && g.b_kmajor) CUBE3D_LAUNCH(true, true, true);

@@ -1,0 +1,288 @@
+"""GPU parity of the linear layer with bias, activation and residual in one product, and of its epilogue's backward pass.
+
+Integers in [-4, 4] (bias and residual too): every sum is exact in fp32 in any order, so results are compared bit for bit after one
+rounding.  Real data: the product's error is the library's stated floor (1e-4 of the largest entry with bf16 and fp8 operands, 2e-5
+with fp32 ones); the activations' slopes stay below 1.13, GELU's evaluation is within 1e-6 (absolute) plus 4e-6 (relative), and
+every stored value is off by half a step of its type."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2105_14450_amd as c3
+from oracle import matmul as om
+from oracle import mlp, numfmt
+from oracle.layout import Cube
+from paper_2105_14450_amd import synth
+from tests import gpu_util as gu
+
+pytestmark = pytest.mark.gpu
+
+ACT = {"none": c3.ACT_NONE, "relu": c3.ACT_RELU, "gelu": c3.ACT_GELU}
+STEP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}
+
+
+def rounded(x, dtype):
+    return numfmt.round_to(x, "bf16") if dtype == "bf16" else x.astype(np.float32).astype(np.float64)
+
+
+class Layer:
+    def __init__(self, q, axis, M, K, N, dtype, dist="int", seed=21, shard="bf16"):
+        self.q, self.axis, self.M, self.K, self.N, self.dtype, self.shard = q, axis, M, K, N, dtype, shard
+        self.cube, self.dist, self.seed = Cube(q, M, K, N, axis), dist, seed
+        inp = synth.linear_inputs(M, K, N, dtype, dist, seed)
+        (x, sx), (w, sw) = inp["X"], inp["W"]
+        self.X, self.W = numfmt.decode(x, dtype, sx), numfmt.decode(w, dtype, sw)
+        self.desc = c3.make_desc(q, M, K, N, in_dtype=gu.CODE[dtype], shard_dtype=gu.CODE[shard],
+                                 in_axis=c3.AXIS_Y if axis == "y" else c3.AXIS_Z, scale_x=sx, scale_w=sw)
+        flat = lambda s: gu.to_device(s.reshape((q ** 3,) + s.shape[3:]))
+        self.x, self.w = flat(self.cube.shard_x(x)), flat(self.cube.shard_w(w))
+        self.b = synth.draw((N,), "int" if dist == "int" else "normal", seed, 31).astype(np.float32)
+        self.bias = gu.to_device(self.cube.shard_bias(self.b, fill=np.nan).astype(np.float32).reshape(q ** 3, -1))
+
+    def rows(self, raw):
+        s = self.cube.shard_y(raw)
+        return gu.to_device(s.reshape((self.q ** 3,) + s.shape[3:]))
+
+    def empty(self, dtype):
+        return gu.empty((self.q ** 3, self.cube.Ms, self.cube.Nb), dtype)
+
+    def matrix(self, t, dtype):
+        a = gu.to_host(t, dtype)
+        return self.cube.unshard_y(a.reshape((self.q,) * 3 + a.shape[1:]))
+
+    def product(self):
+        if not hasattr(self, "z0"):
+            self.z0 = om.forward(self.X, self.W, 4) if self.M * self.K * self.N < 3e8 else self.X @ self.W
+        return self.z0
+
+    def run(self, act, bias=True, residual=None, z=None, in_place=False, stream=None):
+        raw = None
+        if residual:
+            raw = synth.store(synth.draw((self.M, self.N), "int" if self.dist == "int" else "normal", self.seed, 33), residual)[0]
+        res = None if raw is None else self.rows(raw)
+        y, zt = res if in_place else self.empty(self.shard), self.empty(z) if z else None
+        e = c3.make_epilogue(ACT[act], bias=self.bias if bias else None, residual=res, residual_dtype=gu.CODE[residual or "f32"], z=zt,
+                             z_dtype=gu.CODE[z or "f32"])
+        nb = c3.cube3d_epilogue_workspace_bytes(self.desc, c3.OP_FWD)
+        ws = torch.empty(nb + 64, dtype=torch.uint8, device="cuda").fill_(0xFF)
+        c3.virtual_cube_linear_fwd_fused(self.desc, e, self.x, self.w, y, ws[:nb] if nb else None, stream=stream)
+        torch.cuda.synchronize()
+        assert bool((ws[nb:] == 0xFF).all()), "nothing behind the workspace"
+        if res is not None and not in_place:
+            np.testing.assert_array_equal(gu.raw_host(res), gu.raw_host(self.rows(raw)))
+        self.last = (y, zt)
+        return self.matrix(y, self.shard), None if zt is None else self.matrix(zt, z), None if raw is None else numfmt.decode(raw, residual)
+
+    def check(self, act, bias=True, residual=None, z=None, in_place=False):
+        got_y, got_z, res = self.run(act, bias, residual, z, in_place)
+        ref_z = self.product() + (self.b.astype(np.float64) if bias else 0.0)
+        ref_y = (ref_z if act == "none" else mlp.act(ref_z, act)) + (0.0 if res is None else res)
+        what = "q=%d M=%d K=%d N=%d %s %s" % (self.q, self.M, self.K, self.N, self.dtype, act)
+        if self.dist == "int" and act != "gelu":
+            np.testing.assert_array_equal(got_y, rounded(ref_y, self.shard), err_msg=what)
+            if z:
+                np.testing.assert_array_equal(got_z, rounded(ref_z, z), err_msg=what)
+            return
+        floor = 0.0 if self.dist == "int" else (2e-5 if self.dtype == "f32" else 1e-4) * np.abs(self.product()).max() + \
+            2.0 ** -23 * np.abs(self.b).max()
+        if z:
+            assert np.all(np.abs(got_z - ref_z) <= floor + STEP[z] * np.abs(ref_z) * 1.01), what
+        lim = 1.13 * floor + (4e-6 * np.abs(ref_y) + 1e-6 if act == "gelu" else 0.0) + 2.0 ** -23 * (0.0 if res is None else np.abs(res))
+        assert np.all(np.abs(got_y - ref_y) <= lim + STEP[self.shard] * (np.abs(ref_y) + lim) * 1.01), what
+
+
+VARIANTS = [("none", True, None, None), ("relu", True, "bf16", "bf16"), ("relu", False, "f32", "f32"), ("none", False, "bf16", "f32")]
+
+# one token to many, few to many columns, contractions of one to long ones; odd sizes; tile-aligned ones; both directions
+SIZES = [(1, "y", 1, 1, 1), (1, "y", 1, 2048, 256), (1, "z", 1, 100, 1000), (1, "y", 2, 4096, 128), (1, "y", 3, 65, 33), (1, "z", 5, 2056, 520),
+         (1, "y", 16, 1024, 384), (1, "y", 17, 512, 1024), (1, "z", 33, 999, 77), (1, "y", 48, 2048, 640), (1, "y", 64, 4096, 512),
+         (1, "y", 65, 256, 256), (1, "z", 200, 264, 328), (1, "y", 384, 512, 640), (1, "y", 512, 1024, 512), (2, "y", 4, 64, 64),
+         (2, "z", 4, 4096, 512), (2, "y", 16, 8192, 256), (2, "z", 64, 1024, 2048), (2, "y", 36, 30, 28), (2, "z", 256, 512, 768), (2, "y", 1024, 512, 1024),
+         (3, "y", 9, 1152, 576), (3, "z", 333, 198, 279), (3, "y", 999, 384, 1152), (4, "z", 16, 2048, 1024), (4, "y", 64, 1024, 2048),
+         (4, "z", 1024, 512, 1024), (4, "y", 48, 2560, 128), (5, "z", 25, 40, 50)]
+
+
+@pytest.mark.parametrize("q,axis,M,K,N", SIZES)
+@pytest.mark.parametrize("dtype", ["bf16", "fp8_e4m3", "f32"])
+def test_integers(q, axis, M, K, N, dtype):
+    layer = Layer(q, axis, M, K, N, dtype)
+    for act, bias, residual, z in VARIANTS:
+        layer.check(act, bias, residual, z)
+
+
+@pytest.mark.parametrize("dtype,shard", [("bf16", "bf16"), ("bf16", "f32"), ("fp8_e4m3", "bf16"), ("fp8_e4m3", "f32"), ("f32", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("q,axis,M,K,N", [(1, "y", 1, 1024, 512), (1, "z", 7, 520, 264), (2, "y", 16, 2048, 1024), (1, "y", 61, 333, 129), (2, "z", 512, 512, 1024),
+                                          (3, "y", 99, 390, 396), (1, "y", 1536, 1024, 2048)])
+def test_gelu_on_real_data(q, axis, M, K, N, dtype, shard):
+    layer = Layer(q, axis, M, K, N, dtype, "normal", shard=shard)
+    layer.check("gelu", True, "f32", "bf16")
+    layer.check("gelu", False, None, "f32")
+    layer.check("gelu", True, "bf16", None)
+
+
+@pytest.mark.parametrize("q,M,K,N", [(1, 1, 512, 512), (1, 40, 2048, 256), (2, 512, 512, 1024), (1, 130, 100, 70), (3, 999, 384, 1152)])
+@pytest.mark.parametrize("shard", ["bf16", "f32"])
+def test_residual_in_place(q, M, K, N, shard):
+    layer = Layer(q, "y", M, K, N, "bf16", shard=shard)
+    layer.check("relu", True, shard, "bf16", in_place=True)
+    layer.check("none", False, shard, None, in_place=True)
+
+
+@pytest.mark.parametrize("q,M,K,N,dtype", [(4, 8192, 2048, 8192, "bf16"), (4, 8192, 8192, 2048, "bf16"), (2, 4096, 2048, 4096, "fp8_e4m3"),
+                                           (3, 2997, 1152, 4608, "bf16"), (1, 4000, 1600, 2408, "bf16"), (1, 2100, 1000, 1601, "bf16")])
+def test_large(q, M, K, N, dtype):
+    """Against the plain product in fp64 on the device, element by element."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    draw = lambda s, sigma: torch.randn(s, device="cuda", generator=gen).mul_(sigma)
+    T = {"bf16": torch.bfloat16, "fp8_e4m3": torch.float8_e4m3fn}[dtype]
+    sx, sw = (1.0, 1.0) if dtype == "bf16" else (0.01, 0.0002)
+    X, W = (draw((M, K), 1.0) / sx).to(T), (draw((K, N), 0.02) / sw).to(T)
+    R, b = draw((M, N), 1.0).to(torch.bfloat16), draw((N,), 0.1)
+    ref_z = (X.double() @ W.double()) * (sx * sw) + b.double()
+    ref_y = ref_z * torch.special.ndtr(ref_z) + R.double()
+    d = c3.make_desc(q, M, K, N, in_dtype=gu.CODE[dtype], shard_dtype=c3.BF16, scale_x=sx, scale_w=sw)
+    bytes_of = lambda t: t.view(torch.uint8 if dtype == "fp8_e4m3" else torch.int16)
+    x, w, r = gu.device_shards(bytes_of(X), "x", q), gu.device_shards(bytes_of(W), "w", q), gu.device_shards(R, "y", q)
+    bias = torch.empty((q ** 3, N // q ** 2), device="cuda")
+    c3.virtual_cube_scatter(d, c3.OPERAND_BIAS, b, bias)
+    y, z = torch.full_like(r, float("nan")), torch.full_like(r, float("nan"))
+    e = c3.make_epilogue(c3.ACT_GELU, bias=bias, residual=r, residual_dtype=c3.BF16, z=z, z_dtype=c3.BF16)
+    nb = c3.cube3d_epilogue_workspace_bytes(d, c3.OP_FWD)
+    c3.virtual_cube_linear_fwd_fused(d, e, x, w, y, torch.empty(nb, dtype=torch.uint8, device="cuda") if nb else None)
+    Y, Z = torch.empty_like(R), torch.empty_like(R)
+    c3.virtual_cube_assemble(d, c3.OPERAND_Y, y, Y)
+    c3.virtual_cube_assemble(d, c3.OPERAND_Y, z, Z)
+    # (the fp8 codes of the few draws beyond the largest one are NaN: their rows and columns are, and nothing else)
+    floor = 1e-4 * float((ref_z - b).abs().nan_to_num(0.0).max()) + 1e-6
+    for got, ref in ((Z.double(), ref_z), (Y.double(), ref_y)):
+        near = (got - ref).abs() <= 1.13 * floor + 1.01 * 2.0 ** -8 * (ref.abs() + 1.13 * floor)
+        assert bool((near | (got.isnan() & ref.isnan())).all())
+
+
+def test_rows_of_infinities_stay_in_their_row():
+    layer = Layer(1, "y", 40, 256, 128, "f32")
+    layer.x[0, 3, 17] = float("inf")
+    y, z, _ = layer.run("none", True, None, "f32")
+    keep = [k for k in range(40) if k != 3]
+    np.testing.assert_array_equal(y[keep], rounded(layer.product()[keep] + layer.b, "bf16"))
+    assert not np.isfinite(z[3]).any()
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 777 * 8, 264), (5, 40, 24), (16, 8, 8), (64, 1000, 136)])
+def test_weights_that_are_not_finite_stay_in_their_column(M, K, N):
+    """A column of infinities, and nothing read from behind the weights' end or twice where a tile hangs over."""
+    layer = Layer(1, "y", M, K, N, "bf16")
+    w = layer.w.clone()
+    w[0, :, N - 1] = 0x7F80       # +inf
+    layer.w = w
+    layer.x[layer.x == 0] = 0x3F80    # no zeros: 1
+    layer.X = numfmt.decode_bf16(layer.x.cpu().numpy().view(np.uint16)[0])
+    y, _, _ = layer.run("none", True)
+    np.testing.assert_array_equal(y[:, :N - 1], rounded(layer.X @ layer.W[:, :N - 1] + layer.b[:N - 1], "bf16"))
+    assert not np.isfinite(y[:, N - 1]).any()
+
+
+@pytest.mark.parametrize("q,M,K,N", [(2, 16, 4096, 512), (2, 512, 512, 1024), (1, 70, 90, 50)])
+def test_another_stream_and_a_captured_graph(q, M, K, N):
+    layer = Layer(q, "z", M, K, N, "bf16")
+    want, _, _ = layer.run("relu")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got, _, _ = layer.run("relu", stream=side)
+    np.testing.assert_array_equal(got, want)
+    nb = c3.cube3d_epilogue_workspace_bytes(layer.desc, c3.OP_FWD)
+    ws = torch.empty(nb, dtype=torch.uint8, device="cuda") if nb else None
+    e, y = c3.make_epilogue(c3.ACT_RELU, bias=layer.bias), layer.empty("bf16")
+    c3.cube3d_init()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c3.virtual_cube_linear_fwd_fused(layer.desc, e, layer.x, layer.w, y, ws)
+    x0 = layer.x.clone()
+    for turn in range(3):
+        layer.x.copy_(x0 if turn != 1 else x0.flip(1))
+        y.fill_(-1)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = gu.raw_host(y).copy()
+        y.fill_(-1)
+        c3.virtual_cube_linear_fwd_fused(layer.desc, e, layer.x, layer.w, y, ws)
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(replayed, gu.raw_host(y))
+        if turn != 1:
+            np.testing.assert_array_equal(layer.matrix(y, "bf16"), want)
+
+
+def test_too_small_a_workspace_is_refused():
+    layer = Layer(1, "y", 1, 8192, 1024, "bf16")
+    nb = c3.cube3d_epilogue_workspace_bytes(layer.desc, c3.OP_FWD)
+    if nb:
+        e, y = c3.make_epilogue(), layer.empty("bf16")
+        for ws in (None, torch.empty(nb - 1, dtype=torch.uint8, device="cuda")):
+            with pytest.raises(c3.Cube3DError) as err:
+                c3.virtual_cube_linear_fwd_fused(layer.desc, e, layer.x, layer.w, y, ws)
+            assert err.value.status == c3.EWORKSPACE
+
+
+# ---- the backward pass of the epilogue -------------------------------------------------------------
+
+def epilogue_bwd(q, axis, M, N, act, zt, gt, dt, dist="int", with_db=True, in_place=False):
+    cube = Cube(q, M, q, N, axis)
+    d = c3.make_desc(q, M, q, N, in_dtype=c3.BF16, in_axis=c3.AXIS_Y if axis == "y" else c3.AXIS_Z)
+    z_raw, _ = synth.store(synth.draw((M, N), dist, 51, 1, 1.5), zt)
+    g_raw, _ = synth.store(synth.draw((M, N), dist, 51, 2), gt)
+    flat = lambda raw: (lambda s: gu.to_device(s.reshape((q ** 3,) + s.shape[3:])))(cube.shard_y(raw))
+    z, dy = flat(z_raw), flat(g_raw)
+    dz = dy if in_place else gu.empty((q ** 3, cube.Ms, cube.Nb), dt)
+    db = gu.empty((q ** 3, cube.Ns), "f32") if with_db else None
+    nb = c3.cube3d_epilogue_workspace_bytes(d, c3.OP_BIAS_BWD)
+    ws = torch.empty(nb + 64, dtype=torch.uint8, device="cuda").fill_(0xFF)
+    args = (d, ACT[act], gu.CODE[zt], gu.CODE[gt], gu.CODE[dt], z, dy, dz, db, ws[:nb] if with_db else None)
+    c3.virtual_cube_linear_epilogue_bwd(*args)
+    torch.cuda.synchronize()
+    assert bool((ws[nb:] == 0xFF).all())
+    zv, gv = numfmt.decode(z_raw, zt), numfmt.decode(g_raw, gt)
+    want = gv * mlp.act_grad(zv, act)
+    a = gu.to_host(dz, dt)
+    got = cube.unshard_y(a.reshape((q,) * 3 + a.shape[1:]))
+    if act == "relu":
+        np.testing.assert_array_equal(got, rounded(want, dt))
+    else:
+        assert np.all(np.abs(got - want) <= STEP[dt] * 1.01 * np.abs(want) + 5e-6 * np.abs(gv))
+    if with_db:
+        b = gu.to_host(db, "f32").reshape((q,) * 3 + (-1,))
+        for j in range(q):
+            for l in range(q):
+                assert j == l or np.all(b[:, j, l] == 0.0)
+        got_b, want_b = cube.unshard_bias(b), want.sum(axis=0)
+        if act == "relu" and dist == "int":
+            np.testing.assert_array_equal(got_b, want_b)
+        else:       # at most 512 additions on the way of any term, and GELU's slope within 5e-6
+            assert np.all(np.abs(got_b - want_b) <= (512 * 2.0 ** -24 + (5e-6 if act == "gelu" else 0.0)) * np.abs(gv).sum(axis=0) * 1.13)
+    if not in_place:
+        first = [gu.raw_host(t).copy() for t in (dz, db) if t is not None]
+        c3.virtual_cube_linear_epilogue_bwd(*args)
+        torch.cuda.synchronize()
+        for a, t in zip(first, [t for t in (dz, db) if t is not None]):
+            np.testing.assert_array_equal(a, gu.raw_host(t))
+
+
+@pytest.mark.parametrize("q,axis,M,N", [(1, "y", 1, 1), (1, "z", 1, 4096), (1, "y", 3, 7), (1, "y", 1000, 8), (1, "z", 5, 520), (1, "y", 4097, 24), (1, "y", 130, 513),
+                                        (2, "y", 4, 4), (2, "z", 256, 512), (2, "y", 100, 40), (3, "z", 333, 279), (3, "y", 99, 72), (4, "z", 64, 2048),
+                                        (4, "y", 1600, 128), (1, "y", 3000, 1024), (5, "z", 25, 50)])
+@pytest.mark.parametrize("act,dist", [("relu", "int"), ("gelu", "normal")])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_epilogue_bwd(q, axis, M, N, act, dist, dtype):
+    epilogue_bwd(q, axis, M, N, act, dtype, dtype, dtype, dist)
+
+
+@pytest.mark.parametrize("zt", ["f32", "bf16"])
+@pytest.mark.parametrize("gt", ["f32", "bf16"])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [128, 36])
+def test_epilogue_bwd_types(zt, gt, dt, N):
+    for act, dist in (("relu", "int"), ("gelu", "normal")):
+        epilogue_bwd(2, "y", 64, N, act, zt, gt, dt, dist)
+        epilogue_bwd(2, "z", 64, N, act, zt, gt, dt, dist, with_db=False)
+        if gt == dt:
+            epilogue_bwd(1, "z", 64, N, act, zt, gt, dt, dist, in_place=True)
