@@ -107,7 +107,6 @@ size_t workspace_for(const GemmArgs &a)
 // The first kernel family that takes the product: tile-aligned sizes, then any size, then element by element.
 int run_gemm(const GemmArgs &a)
 {
-    if (a.epilogue) return gemm_generic(a);
     const FastPlan plan = gemm_fast_plan(a);
     const size_t need = gemm_fast_workspace(a, plan);
     if (need > 0 && (!a.workspace || a.workspace_bytes < need)) return CUBE3D_EWORKSPACE;

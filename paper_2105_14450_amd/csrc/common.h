@@ -133,6 +133,9 @@ int gemm_edge(const GemmArgs &g);
 // Whether its ring kernel takes a tile-aligned product and is safely below `us` microseconds by its estimate.
 bool gemm_edge_takes_less(const GemmArgs &g, double us);
 
+// Consecutive output columns that lie side by side and aligned in every array placed like the output, and in the bias (8, 4, 2, 1).
+void epilogue_pieces(const GemmArgs &g, int *output, int *bias);
+
 // Tuned bf16 / fp8 path.  What it runs a product on: a pure function of the shape, made once per call.
 struct FastPlan {
     int tile;     // 256 or 128 (square output tile); 0 = not supported by the tuned kernel, or not the fastest
@@ -143,6 +146,7 @@ size_t gemm_fast_workspace(const GemmArgs &g, const FastPlan &plan);
 int gemm_fast(const GemmArgs &g, const FastPlan &plan);      // CUBE3D_ENOTIMPL where plan.tile is 0
 // Launch of the tuned kernel's map-addressed instantiations (tile = 256 or 128, chosen by gemm_fast).
 int gemm_fast_mapped(const GemmArgs &g, int tile);
+int gemm_fast_epilogue(const GemmArgs &g, int tile);      // with what follows the product
 
 // Geometry of the virtual cube and the data-movement kernels over it.
 struct CubeGeom {

@@ -111,6 +111,7 @@ int make_plan(const GemmArgs &g, Plan *plan)
     if (g.Mo < 1 || g.No < 1 || g.Kc < 1 || g.batch < 1 || (!g.a_kmajor && g.b_kmajor)) return CUBE3D_ENOTIMPL;
     if (g.Mo > MAX_EXTENT || g.No > MAX_EXTENT || g.Kc > MAX_EXTENT) return CUBE3D_ENOTIMPL;
     if (g.maps && g.batch != 1) return CUBE3D_ENOTIMPL;
+    if (g.epilogue && (!g.maps || !g.a_kmajor || g.b_kmajor)) return CUBE3D_EINVAL;
     if ((g.Mo + 63) / 64 > 65535 || g.batch > 65535) return CUBE3D_ENOTIMPL;   // refused by gemm_generic
     Params &p = plan->params;
     p = Params{};
@@ -175,7 +176,20 @@ int make_plan(const GemmArgs &g, Plan *plan)
     return CUBE3D_OK;
 }
 
+EpilogueParams epilogue_params(const GemmArgs &g, const Params &p)
+{
+    EpilogueParams x{{p}, *g.epilogue, 1, 1};
+    epilogue_pieces(g, &x.piece, &x.bias_piece);
+    return x;
+}
+
 }  // namespace edge
+
+void epilogue_pieces(const GemmArgs &g, int *output, int *bias)
+{
+    *output = (int)piece_of(g.maps->c_n, g.maps->c_m, g.No, 0, 8);
+    *bias = (int)piece_of(g.maps->bias_n, plain_map(0), g.No, 0, 8);
+}
 
 namespace {
 

@@ -189,6 +189,7 @@ size_t gemm_fast_workspace(const GemmArgs &g, const FastPlan &pl)
 int gemm_fast(const GemmArgs &g, const FastPlan &pl)
 {
     if (pl.tile == 0) return CUBE3D_ENOTIMPL;
+    if (g.epilogue) return gemm_fast_epilogue(g, pl.tile);
     if (g.maps) return gemm_fast_mapped(g, pl.tile);
     const bool f32 = g.out_dtype == CUBE3D_F32;
     if (g.in_dtype == CUBE3D_FP8_E4M3) {

@@ -36,7 +36,7 @@
 #include <mutex>
 #include <type_traits>
 
-#include "common.h"
+#include "gemm_epilogue.h"
 
 namespace cube3d {
 namespace mfk {
@@ -243,12 +243,22 @@ struct Params {
 #endif
 };
 
+// The same of a product with what follows it (MAPPED, forward layout): names as TileEpilogue reads them.
+struct EpilogueParams : Params {
+    int Mo, No, out_f32;
+    Epilogue e;
+    int piece, bias_piece;
+};
+
 // TOut: float or unsigned short (bf16 bits).  MAPPED: operands, output and the optional bias are
 // addressed through p.maps (a cube of shards read in place) instead of leading dimensions.
-// The number of K-tiles per workgroup (p.nk) must be a positive multiple of NSTAGE.
-template <typename E, int BM, int BN, int BKB, int NSTAGE, bool AK, bool BKM, typename TOut, bool MAPPED = false>
-__global__ __launch_bounds__(256, (BM * BN <= 128 * 128) ? 2 : 1) void gemm_mfma_kernel(const Params p)
+// The number of K-tiles per workgroup (p.nk) must be a positive multiple of NSTAGE.  P = EpilogueParams: with what
+// follows the product.
+template <typename E, int BM, int BN, int BKB, int NSTAGE, bool AK, bool BKM, typename TOut, bool MAPPED = false, typename P = Params>
+__global__ __launch_bounds__(256, (BM * BN <= 128 * 128) ? 2 : 1) void gemm_mfma_kernel(const P p)
 {
+    constexpr bool EPI = !std::is_same<P, Params>::value;
+    static_assert(!EPI || (MAPPED && AK && !BKM), "the forward product over the cube");
     typedef typename E::Elem Elem;
     typedef typename E::FragI FragI;
     using ATile = typename std::conditional<AK, KMajorTile<E, BM, BKB>, MNMajorTile<E, BM, BKB>>::type;
@@ -281,7 +291,7 @@ __global__ __launch_bounds__(256, (BM * BN <= 128 * 128) ? 2 : 1) void gemm_mfma
     // The optional bias belongs to the forward product (Algorithm 7 follows Algorithm 1): only the
     // map-addressed kernel of that layout stages and adds it; the launcher sends a bias with any other
     // layout to the kernels for any size.
-    constexpr bool BIAS = MAPPED && AK && !BKM;
+    constexpr bool BIAS = MAPPED && AK && !BKM && !EPI;
     constexpr int STRIP_BYTES = 32 * ROWB;
     constexpr int EPI_BYTES = NBUF * STRIP_BYTES;
     static_assert(ROWB == 128 || ROWB == 256, "strip rows of 8 or 16 slots");
@@ -788,7 +798,10 @@ __global__ __launch_bounds__(256, (BM * BN <= 128 * 128) ? 2 : 1) void gemm_mfma
     constexpr int RPP = 64 / LPR;             // rows per pass
     constexpr int NPASS = 32 / RPP;           // passes (16-byte loads and global stores) per strip
     constexpr int NSTRIP = TM * (TN / JH);    // strips per wavefront
-    constexpr int STORES = NSTRIP * NPASS;    // global stores per wavefront
+    typedef TileEpilogue<32, f32x16, TM, TN> Fused;
+    static_assert(!EPI || Fused::BYTES <= EPI_BYTES, "room for the strip");
+    // global stores per wavefront (EPI: those of the result; waits that count on fewer stores than there are wait for more)
+    constexpr int STORES = EPI ? TM * TN * 32 * 32 / 64 / (16 / ESZ) : NSTRIP * NPASS;
     constexpr int RP256 = 256 / ROWB;         // strip rows per 256 bytes of LDS (all banks once)
     auto epilogue_impl = [&](auto scaled_c, int64_t em0, int64_t en0, int ebatch, int esplit) {
         constexpr bool scaled = decltype(scaled_c)::value;   // alpha != 1: one more multiply per element
@@ -920,6 +933,10 @@ __global__ __launch_bounds__(256, (BM * BN <= 128 * 128) ? 2 : 1) void gemm_mfma
     };
 
     auto epilogue = [&](int64_t em0, int64_t en0, int ebatch, int esplit) {
+        if constexpr (EPI) {
+            Fused::store(p, acc, smem + EPI_BASE + wave * EPI_BYTES, (int)em0 + wm * WM, (int)en0 + wn * WN, lane_id);
+            return;
+        }
         if (p.alpha == 1.f) epilogue_impl(std::false_type{}, em0, en0, ebatch, esplit);
         else epilogue_impl(std::true_type{}, em0, en0, ebatch, esplit);
     };
@@ -989,7 +1006,7 @@ template <typename E, int BM, int BN, int BKB, int NSTAGE, bool AK, bool BKM> co
 // the default limit.  Done once per device, under a lock (the flags are the only state the product
 // kernels keep); registered with kernel_setups() so that cube3d_init() can run it before the first
 // launch (a first launch from inside a stream capture would otherwise do it there).
-template <typename E, int BM, int BN, int BKB, int NSTAGE, bool AK, bool BKM, typename TOut, bool MAPPED> struct CfgSetup {
+template <typename E, int BM, int BN, int BKB, int NSTAGE, bool AK, bool BKM, typename TOut, bool MAPPED, typename P> struct CfgSetup {
     static int run()
     {
         static std::mutex mu;
@@ -1000,7 +1017,7 @@ template <typename E, int BM, int BN, int BKB, int NSTAGE, bool AK, bool BKM, ty
         if (done.load(std::memory_order_acquire) & bit) return CUBE3D_OK;
         std::lock_guard<std::mutex> lock(mu);
         if (done.load(std::memory_order_relaxed) & bit) return CUBE3D_OK;
-        auto kern = gemm_mfma_kernel<E, BM, BN, BKB, NSTAGE, AK, BKM, TOut, MAPPED>;
+        auto kern = gemm_mfma_kernel<E, BM, BN, BKB, NSTAGE, AK, BKM, TOut, MAPPED, P>;
         if (hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize,
                                 cfg_lds_bytes<E, BM, BN, BKB, NSTAGE, AK, BKM>()) != hipSuccess) {
             (void)hipGetLastError();
@@ -1017,16 +1034,16 @@ template <typename E, int BM, int BN, int BKB, int NSTAGE, bool AK, bool BKM, ty
 
 // Launch one configuration.  splits > 1: every split writes its own fp32 partial result
 // [batch][split][Mo][No] to `out` (then out_ld = No); splits == 1: `out` is the final C.
-template <typename E, int BM, int BN, int BKB, int NSTAGE, bool AK, bool BKM, typename TOut, bool MAPPED = false>
+template <typename E, int BM, int BN, int BKB, int NSTAGE, bool AK, bool BKM, typename TOut, bool MAPPED = false, typename P = Params>
 int launch_cfg(const GemmArgs &g, int splits, void *out, int64_t out_ld, int64_t out_batch_stride, int64_t out_split_stride,
                float alpha)
 {
     constexpr int LDS = cfg_lds_bytes<E, BM, BN, BKB, NSTAGE, AK, BKM>();
-    using Setup = CfgSetup<E, BM, BN, BKB, NSTAGE, AK, BKM, TOut, MAPPED>;
+    using Setup = CfgSetup<E, BM, BN, BKB, NSTAGE, AK, BKM, TOut, MAPPED, P>;
     (void)&Setup::registrar;   // instantiates the registration
-    auto kern = gemm_mfma_kernel<E, BM, BN, BKB, NSTAGE, AK, BKM, TOut, MAPPED>;
+    auto kern = gemm_mfma_kernel<E, BM, BN, BKB, NSTAGE, AK, BKM, TOut, MAPPED, P>;
     if (const int rc = Setup::run(); rc != CUBE3D_OK) return rc;
-    Params p;
+    P p;
     p.A = g.A;
     p.B = g.B;
     p.C = out;
@@ -1047,6 +1064,13 @@ int launch_cfg(const GemmArgs &g, int splits, void *out, int64_t out_ld, int64_t
             prepare_axis_map(*m);
         p.ka = make_kwalk(g.maps->a_k, BKB / E::ELT);
         p.kb = make_kwalk(g.maps->b_k, BKB / E::ELT);
+    }
+    if constexpr (!std::is_same<P, Params>::value) {
+        p.Mo = (int)g.Mo;
+        p.No = (int)g.No;
+        p.out_f32 = sizeof(TOut) == 4;
+        p.e = *g.epilogue;
+        epilogue_pieces(g, &p.piece, &p.bias_piece);
     }
     p.y_items = g.batch * splits;
 #ifdef CUBE3D_PROFILE
