@@ -107,6 +107,13 @@ size_t workspace_for(const GemmArgs &a)
 // The first kernel family that takes the product: tile-aligned sizes, then any size, then element by element.
 int run_gemm(const GemmArgs &a)
 {
+    if (a.epilogue) {
+        if (const int splits = gemm_rows_plan(a); splits > 0) {
+            const size_t need = gemm_rows_workspace(a, splits);
+            if (need > 0 && (!a.workspace || a.workspace_bytes < need)) return CUBE3D_EWORKSPACE;
+            return gemm_rows(a, splits);
+        }
+    }
     const FastPlan plan = gemm_fast_plan(a);
     const size_t need = gemm_fast_workspace(a, plan);
     if (need > 0 && (!a.workspace || a.workspace_bytes < need)) return CUBE3D_EWORKSPACE;
@@ -155,14 +162,14 @@ ShardMaps shard_maps(const CubeGeom &g)
     return m;
 }
 
-// One product over the whole cube with the shards read and written in place.
-int run_cube_product(const cube3d_desc *d, int op, const void *A, const void *B, const void *bias, void *C, void *stream,
-                     const Epilogue *epilogue = nullptr)
+// One product over the whole cube with the shards read and written in place: its description (with the maps in *mp), without
+// workspace or epilogue.
+int build_cube_product(const cube3d_desc *d, int op, const void *A, const void *B, const void *bias, void *C, void *stream, GemmMaps *maps,
+                       GemmArgs *out)
 {
     CubeGeom g;
     int rc = check_desc(d, &g);
     if (rc != CUBE3D_OK) return rc;
-    if (!A || !B || !C || misaligned(A) || misaligned(B) || misaligned(C) || misaligned(bias)) return CUBE3D_EINVAL;
     if (g.M >= (1ll << 31) || g.K >= (1ll << 31) || g.N >= (1ll << 31)) return CUBE3D_ESHAPE;
     const ShardMaps sm = shard_maps(g);
     const bool fp8 = d->in_dtype == CUBE3D_FP8_E4M3;
@@ -197,8 +204,20 @@ int run_cube_product(const cube3d_desc *d, int op, const void *A, const void *B,
     default: return CUBE3D_EINVAL;
     }
     if (mp.bias == nullptr) mp.bias_n = sm.bn;
-    a.maps = &mp;
-    a.epilogue = epilogue;
+    *maps = mp;
+    a.maps = maps;
+    *out = a;
+    return CUBE3D_OK;
+}
+
+int run_cube_product(const cube3d_desc *d, int op, const void *A, const void *B, const void *bias, void *C, void *stream)
+{
+    const int rc = check_desc(d, nullptr);
+    if (rc != CUBE3D_OK) return rc;
+    if (!A || !B || !C || misaligned(A) || misaligned(B) || misaligned(C) || misaligned(bias)) return CUBE3D_EINVAL;
+    GemmMaps maps;
+    GemmArgs a;
+    if (const int e = build_cube_product(d, op, A, B, bias, C, stream, &maps, &a); e != CUBE3D_OK) return e;
     return run_gemm(a);
 }
 
@@ -682,7 +701,13 @@ size_t cube3d_epilogue_workspace_bytes(const cube3d_desc *desc, int op)
     CubeGeom g;
     if (check_desc(desc, &g) != CUBE3D_OK) return 0;
     if (op == CUBE3D_OP_BIAS_BWD) return epilogue_bwd_workspace(g);
-    return 0;
+    if (op != CUBE3D_OP_FWD) return 0;
+    const Epilogue any{};
+    GemmMaps maps;
+    GemmArgs a;
+    if (build_cube_product(desc, op, nullptr, nullptr, nullptr, nullptr, nullptr, &maps, &a) != CUBE3D_OK) return 0;
+    a.epilogue = &any;
+    return gemm_rows_workspace(a, gemm_rows_plan(a));
 }
 
 int virtual_cube_linear_fwd_fused(const cube3d_desc *desc, const cube3d_epilogue *epilogue, const void *X_shards,
@@ -701,8 +726,17 @@ int virtual_cube_linear_fwd_fused(const cube3d_desc *desc, const cube3d_epilogue
     if (epilogue->residual == Y_shards && Y_shards && epilogue->residual_dtype != desc->shard_dtype) return CUBE3D_EINVAL;
     const Epilogue e{epilogue->activation, epilogue->residual && epilogue->residual_dtype == CUBE3D_F32,
                      epilogue->z && epilogue->z_dtype == CUBE3D_F32, epilogue->residual, epilogue->z};
-    (void)workspace_bytes;
-    return run_cube_product(desc, CUBE3D_OP_FWD, X_shards, W_shards, epilogue->bias_diag, Y_shards, stream, &e);
+    if (!X_shards || !W_shards || !Y_shards || misaligned(X_shards) || misaligned(W_shards) || misaligned(Y_shards) ||
+        misaligned(epilogue->bias_diag))
+        return CUBE3D_EINVAL;
+    GemmMaps maps;
+    GemmArgs a;
+    rc = build_cube_product(desc, CUBE3D_OP_FWD, X_shards, W_shards, epilogue->bias_diag, Y_shards, stream, &maps, &a);
+    if (rc != CUBE3D_OK) return rc;
+    a.epilogue = &e;
+    a.workspace = workspace;
+    a.workspace_bytes = workspace_bytes;
+    return run_gemm(a);
 }
 
 int virtual_cube_linear_epilogue_bwd(const cube3d_desc *desc, int kind, int z_dtype, int dy_dtype, int dz_dtype,

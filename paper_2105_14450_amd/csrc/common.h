@@ -136,6 +136,11 @@ bool gemm_edge_takes_less(const GemmArgs &g, double us);
 // Consecutive output columns that lie side by side and aligned in every array placed like the output, and in the bias (8, 4, 2, 1).
 void epilogue_pieces(const GemmArgs &g, int *output, int *bias);
 
+// Few rows with what follows the product: runs of the contraction (0: not this kernel's), scratch in bytes, launch.
+int gemm_rows_plan(const GemmArgs &g);
+size_t gemm_rows_workspace(const GemmArgs &g, int splits);
+int gemm_rows(const GemmArgs &g, int splits);
+
 // Tuned bf16 / fp8 path.  What it runs a product on: a pure function of the shape, made once per call.
 struct FastPlan {
     int tile;     // 256 or 128 (square output tile); 0 = not supported by the tuned kernel, or not the fastest

@@ -190,7 +190,11 @@ __global__ __launch_bounds__(256, T == 128 || GB == 1 ? 2 : 3) void CUBE3D_EDGE_
                 for (int e = 0; e < 4; ++e) x[4 * half + e] = t[e] * p.alpha + bias[4 * half + e];
             }
 #if CUBE3D_EDGE_EPILOGUE
-            if (p.piece == 8) EpilogueRun<8>::apply(p.e, x, C, p.out_f32, row_off + col_off);
+            if (p.piece == 8) {
+                EpilogueRun<8>::Residual residual;
+                EpilogueRun<8>::load<ANY>(p.e, row_off + col_off, residual);
+                EpilogueRun<8>::apply<ANY>(p.e, x, residual, C, p.out_f32, row_off + col_off);
+            }
             else EpilogueRun<8>::apply_some(p.e, x, C, p.out_f32, row_off, p.maps.c_n, col, p.No);
 #else
             if (p.out_wide) {

@@ -798,8 +798,9 @@ __global__ __launch_bounds__(256, (BM * BN <= 128 * 128) ? 2 : 1) void gemm_mfma
     constexpr int RPP = 64 / LPR;             // rows per pass
     constexpr int NPASS = 32 / RPP;           // passes (16-byte loads and global stores) per strip
     constexpr int NSTRIP = TM * (TN / JH);    // strips per wavefront
-    typedef TileEpilogue<32, f32x16, TM, TN> Fused;
-    static_assert(!EPI || Fused::BYTES <= EPI_BYTES, "room for the strip");
+    constexpr int FUSED_ROOM = 8192;          // strips of 32 rows x 64 columns
+    typedef TileEpilogue<32, f32x16, TM, TN, FUSED_ROOM, true, true> Fused;
+    static_assert(!EPI || EPI_BASE + WAVES * FUSED_ROOM <= (EPI_SEPARATE ? 160 * 1024 : NSTAGE * STAGE_BYTES), "room for the strips");
     // global stores per wavefront (EPI: those of the result; waits that count on fewer stores than there are wait for more)
     constexpr int STORES = EPI ? TM * TN * 32 * 32 / 64 / (16 / ESZ) : NSTRIP * NPASS;
     constexpr int RP256 = 256 / ROWB;         // strip rows per 256 bytes of LDS (all banks once)
@@ -934,7 +935,7 @@ __global__ __launch_bounds__(256, (BM * BN <= 128 * 128) ? 2 : 1) void gemm_mfma
 
     auto epilogue = [&](int64_t em0, int64_t en0, int ebatch, int esplit) {
         if constexpr (EPI) {
-            Fused::store(p, acc, smem + EPI_BASE + wave * EPI_BYTES, (int)em0 + wm * WM, (int)en0 + wn * WN, lane_id);
+            Fused::store(p, acc, smem + EPI_BASE + wave * FUSED_ROOM, (int)em0 + wm * WM, (int)en0 + wn * WN, lane_id);
             return;
         }
         if (p.alpha == 1.f) epilogue_impl(std::false_type{}, em0, en0, ebatch, esplit);

@@ -340,12 +340,12 @@ template <typename E, int TM, int TN, int NST> int ring_layout(const GemmArgs &g
     p.by_group = make_divisor(p.group_m * p.tiles_n);
     p.by_last = make_divisor(p.tiles_m % p.group_m ? p.tiles_m % p.group_m : p.group_m);
     const dim3 grid((unsigned)(items < places ? items : places)), block(512);
-    if (g.epilogue) {
-        hipLaunchKernelGGL((gemm_ring_epilogue_kernel<E, TM, TN, NST, true, false, false>), grid, block, 0, g.stream, epilogue_params(g, p));
-        return launch_status();
-    }
     auto launch = [&](auto stream) {
         constexpr bool S = decltype(stream)::value;
+        if (g.epilogue) {
+            hipLaunchKernelGGL((gemm_ring_epilogue_kernel<E, TM, TN, NST, true, false, S>), grid, block, 0, g.stream, epilogue_params(g, p));
+            return launch_status();
+        }
         if (g.a_kmajor && g.b_kmajor) hipLaunchKernelGGL((gemm_ring_kernel<E, TM, TN, NST, true, true, S>), grid, block, 0, g.stream, p);
         else if (g.a_kmajor) hipLaunchKernelGGL((gemm_ring_kernel<E, TM, TN, NST, true, false, S>), grid, block, 0, g.stream, p);
         else hipLaunchKernelGGL((gemm_ring_kernel<E, TM, TN, NST, false, false, S>), grid, block, 0, g.stream, p);

@@ -20,7 +20,7 @@ __global__ __launch_bounds__(512, 2 * ring_per_cu(TM, TN, NST)) void CUBE3D_RING
     constexpr int STRIP = ring_strip(TN);
     static_assert(RingOutput<M, NBM, NBN, 2, false, STREAM>::BYTES <= STRIP && RingOutput<M, NBM, NBN, 4, false, STREAM>::BYTES <= STRIP, "room for the output strips");
 #if CUBE3D_RING_EPILOGUE
-    typedef TileEpilogue<SIDE, Acc, NBM, NBN> Output;
+    typedef TileEpilogue<SIDE, Acc, NBM, NBN, STRIP, (NBM * NBN < 8), STREAM> Output;
     static_assert(Output::BYTES <= STRIP, "room for the output strips");
 #else
     typedef std::integral_constant<int, 2> I2;

@@ -224,6 +224,21 @@ def test_too_small_a_workspace_is_refused():
             assert err.value.status == c3.EWORKSPACE
 
 
+# Few rows and long contractions: split over workgroups and joined.  One row to 64, shards that end inside a k-step of 32, a
+# contraction that does, columns that end inside a strip of 128, one run and many
+@pytest.mark.parametrize("q,axis,M,K,N", [(1, "y", 1, 6144, 8), (1, "z", 15, 6152, 136), (1, "y", 16, 16384, 128), (1, "y", 17, 8200, 264), (1, "z", 32, 6176, 1000),
+                                          (1, "y", 33, 7000, 392), (1, "y", 49, 12288, 512), (1, "z", 64, 6208, 8192), (2, "y", 4, 6160, 96), (2, "z", 60, 8208, 544),
+                                          (3, "y", 9, 6168, 72), (3, "z", 54, 6408, 648), (4, "y", 16, 6432, 1152), (4, "z", 64, 8224, 256), (1, "y", 5, 40000, 256)])
+@pytest.mark.parametrize("dtype,shard", [("bf16", "bf16"), ("fp8_e4m3", "bf16"), ("bf16", "f32")])
+def test_few_rows(q, axis, M, K, N, dtype, shard):
+    layer = Layer(q, axis, M, K, N, dtype, shard=shard)
+    for act, bias, residual, z in VARIANTS:
+        layer.check(act, bias, residual, z)
+    layer.check("relu", True, shard, None, in_place=True)
+    first = layer.run("none", True)[0]
+    np.testing.assert_array_equal(first, layer.run("none", True)[0])
+
+
 # ---- the backward pass of the epilogue -------------------------------------------------------------
 
 def epilogue_bwd(q, axis, M, N, act, zt, gt, dt, dist="int", with_db=True, in_place=False):
