@@ -7,13 +7,18 @@
 //
 // A row's columns lie in q blocks, q * Ri processors apart: row and column offsets come from index maps, so that the rows of
 // the whole cube are one matrix here.
+#include <type_traits>
+
 #include "activation.h"
 
 namespace cube3d {
 
 namespace {
 
+constexpr int VECTORS = 5;      // post_gamma, post_beta, gate, pre_gamma, pre_beta
+
 // ---- any size: one workgroup per row, the row read again for every step ---------------------------------
+// V consecutive columns at a time: eight where they lie side by side in every array, else one.
 
 constexpr int ROW_LANES = 256;
 
@@ -39,12 +44,33 @@ template <int K, int THREADS> __device__ __forceinline__ void row_sum(float (&x)
     }
 }
 
-__device__ __forceinline__ float vector_at(const float *v, const AxisMap &m, int c, float absent)
+template <typename T, int V> struct __attribute__((aligned(sizeof(T) * V))) Columns {
+    T v[V];
+};
+
+template <typename T, int V> __device__ __forceinline__ void get(const T *from, int64_t at, float (&x)[V])
 {
-    return v ? v[axis_offset_fast(m, c)] : absent;
+    const Columns<T, V> c = *reinterpret_cast<const Columns<T, V> *>(from + at);
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = to_f32<T>(c.v[e]);
+}
+template <typename T, int V> __device__ __forceinline__ void put(T *to, int64_t at, const float (&x)[V])
+{
+    Columns<T, V> c;
+#pragma unroll
+    for (int e = 0; e < V; ++e) c.v[e] = from_f32<T>(x[e]);
+    *reinterpret_cast<Columns<T, V> *>(to + at) = c;
+}
+// V elements of a vector in diagonal storage
+template <int V> __device__ __forceinline__ void vector_at(const float *v, int64_t at, float absent, float (&x)[V])
+{
+    if (v) get<float, V>(v, at, x);
+    else
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] = absent;
 }
 
-template <typename TS, typename TB> __global__ __launch_bounds__(ROW_LANES) void norm_fwd_rows_kernel(const NormArgs a)
+template <typename TS, typename TB, int V> __global__ __launch_bounds__(ROW_LANES) void norm_fwd_rows_kernel(const NormArgs a)
 {
     __shared__ float lds[2][ROW_LANES / 64 * 4];
     const TS *x = static_cast<const TS *>(a.x);
@@ -56,102 +82,133 @@ template <typename TS, typename TB> __global__ __launch_bounds__(ROW_LANES) void
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const int64_t at = axis_offset_fast(a.row, row);
         float post_mean = 0.f, post_rstd = 0.f, pre_mean = 0.f, pre_rstd = 0.f;
-        if (a.post_kind != CUBE3D_NORM_NONE) {
+        // sum over the row of f(value), f of V columns at a time
+        auto total = [&](auto &&values, auto &&f) {
             float s[1] = {0.f};
-            if (a.post_kind == CUBE3D_NORM_LAYER) {
-                for (int c = threadIdx.x; c < a.cols; c += ROW_LANES) s[0] += to_f32<TB>(u[at + axis_offset_fast(a.col, c)]);
-                row_sum<1, ROW_LANES>(s, lds, slot);
-                post_mean = s[0] * inv;
-                s[0] = 0.f;
-            }
-            for (int c = threadIdx.x; c < a.cols; c += ROW_LANES) {
-                const float d = to_f32<TB>(u[at + axis_offset_fast(a.col, c)]) - post_mean;
-                s[0] = fmaf(d, d, s[0]);
+            for (int c = threadIdx.x * V; c < a.cols; c += ROW_LANES * V) {
+                float v[V];
+                values(c, at + axis_offset_fast(a.col, c), v);
+#pragma unroll
+                for (int e = 0; e < V; ++e) s[0] += f(v[e]);
             }
             row_sum<1, ROW_LANES>(s, lds, slot);
-            post_rstd = 1.f / sqrtf(s[0] * inv + a.post_eps);
+            return s[0];
+        };
+        if (a.post_kind != CUBE3D_NORM_NONE) {
+            auto block = [&](int, int64_t i, float (&v)[V]) { get<TB, V>(u, i, v); };
+            if (a.post_kind == CUBE3D_NORM_LAYER) post_mean = total(block, [](float v) { return v; }) * inv;
+            post_rstd = 1.f / sqrtf(total(block, [&](float v) { return (v - post_mean) * (v - post_mean); }) * inv + a.post_eps);
         }
-        // r of one column, in fp32
-        auto stream = [&](int c, int64_t i) {
-            const float xv = to_f32<TS>(x[i]);
-            if (!a.u) return xv;
-            float v = to_f32<TB>(u[i]);
-            if (a.post_kind != CUBE3D_NORM_NONE)
-                v = (v - post_mean) * post_rstd * vector_at(a.p.post_gamma, a.vec, c, 1.f) + vector_at(a.p.post_beta, a.vec, c, 0.f);
-            return xv + a.scale * vector_at(a.p.gate, a.vec, c, 1.f) * v;
+        // r of V columns, in fp32
+        auto stream = [&](int c, int64_t i, float (&v)[V]) {
+            get<TS, V>(x, i, v);
+            if (!a.u) return;
+            const int64_t vec = axis_offset_fast(a.vec, c);
+            float w[V], gate[V];
+            get<TB, V>(u, i, w);
+            if (a.post_kind != CUBE3D_NORM_NONE) {
+                float gamma[V], beta[V];
+                vector_at<V>(a.p.post_gamma, vec, 1.f, gamma);
+                vector_at<V>(a.p.post_beta, vec, 0.f, beta);
+#pragma unroll
+                for (int e = 0; e < V; ++e) w[e] = (w[e] - post_mean) * post_rstd * gamma[e] + beta[e];
+            }
+            vector_at<V>(a.p.gate, vec, 1.f, gate);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] += a.scale * gate[e] * w[e];
         };
         if (a.pre_kind != CUBE3D_NORM_NONE) {
-            float s[1] = {0.f};
-            if (a.pre_kind == CUBE3D_NORM_LAYER) {
-                for (int c = threadIdx.x; c < a.cols; c += ROW_LANES) s[0] += stream(c, at + axis_offset_fast(a.col, c));
-                row_sum<1, ROW_LANES>(s, lds, slot);
-                pre_mean = s[0] * inv;
-                s[0] = 0.f;
-            }
-            for (int c = threadIdx.x; c < a.cols; c += ROW_LANES) {
-                const float d = stream(c, at + axis_offset_fast(a.col, c)) - pre_mean;
-                s[0] = fmaf(d, d, s[0]);
-            }
-            row_sum<1, ROW_LANES>(s, lds, slot);
-            pre_rstd = 1.f / sqrtf(s[0] * inv + a.pre_eps);
+            if (a.pre_kind == CUBE3D_NORM_LAYER) pre_mean = total(stream, [](float v) { return v; }) * inv;
+            pre_rstd = 1.f / sqrtf(total(stream, [&](float v) { return (v - pre_mean) * (v - pre_mean); }) * inv + a.pre_eps);
         }
-        for (int c = threadIdx.x; c < a.cols; c += ROW_LANES) {
+        for (int c = threadIdx.x * V; c < a.cols; c += ROW_LANES * V) {
             const int64_t i = at + axis_offset_fast(a.col, c);
-            const float v = stream(c, i);
-            if (n) n[i] = from_f32<TB>((v - pre_mean) * pre_rstd * vector_at(a.p.pre_gamma, a.vec, c, 1.f) +
-                                       vector_at(a.p.pre_beta, a.vec, c, 0.f));
-            if (r) r[i] = from_f32<TS>(v);      // (behind the last read of x: r may be x)
+            float v[V];
+            stream(c, i, v);
+            if (n) {
+                const int64_t vec = axis_offset_fast(a.vec, c);
+                float y[V], gamma[V], beta[V];
+                vector_at<V>(a.p.pre_gamma, vec, 1.f, gamma);
+                vector_at<V>(a.p.pre_beta, vec, 0.f, beta);
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = (v[e] - pre_mean) * pre_rstd * gamma[e] + beta[e];
+                put<TB, V>(n, i, y);
+            }
+            if (r) put<TS, V>(r, i, v);      // (behind the last read of x: r may be x)
         }
         if (a.stats_out && threadIdx.x == 0)
             *reinterpret_cast<f32x4 *>(a.stats_out + 4 * row) = f32x4{post_mean, post_rstd, pre_mean, pre_rstd};
     }
 }
 
-// What a column of the backward pass is made of.  (m1, m2: mean(t) and mean(t r^) of the norm ahead of the next block, m3, m4 of
-// the norm behind the block.)
-struct ColumnParams {
-    float post_gamma, post_beta, gate, pre_gamma;
+// What V columns of the backward pass are multiplied with.
+template <int V> struct ColumnParams {
+    float post_gamma[V], post_beta[V], gate[V], pre_gamma[V];
+    __device__ __forceinline__ void look_up(const NormArgs &a, int c)
+    {
+        const int64_t vec = axis_offset_fast(a.vec, c);
+        vector_at<V>(a.p.post_gamma, vec, 1.f, post_gamma);
+        vector_at<V>(a.p.post_beta, vec, 0.f, post_beta);
+        vector_at<V>(a.p.gate, vec, 1.f, gate);
+        vector_at<V>(a.p.pre_gamma, vec, 1.f, pre_gamma);
+    }
 };
 
-__device__ __forceinline__ ColumnParams column_params(const NormArgs &a, int c)
-{
-    return ColumnParams{vector_at(a.p.post_gamma, a.vec, c, 1.f), vector_at(a.p.post_beta, a.vec, c, 0.f),
-                        vector_at(a.p.gate, a.vec, c, 1.f), vector_at(a.p.pre_gamma, a.vec, c, 1.f)};
-}
-
 // Row sums of the backward pass: scalars[row] = mean(t), mean(t r^), mean(tp), mean(tp u^)
-template <typename TS, typename TB> __global__ __launch_bounds__(ROW_LANES) void norm_bwd_rows_kernel(const NormArgs a, float *__restrict__ scalars)
+template <typename TS, typename TB, int V>
+__global__ __launch_bounds__(ROW_LANES) void norm_bwd_rows_kernel(const NormArgs a, float *__restrict__ scalars)
 {
     __shared__ float lds[2][ROW_LANES / 64 * 4];
     const TS *dr = static_cast<const TS *>(a.dr), *r = static_cast<const TS *>(a.x);
     const TB *dn = static_cast<const TB *>(a.dn), *u = static_cast<const TB *>(a.u);
+    const bool pre = a.pre_kind != CUBE3D_NORM_NONE;
     const float inv = 1.f / (float)a.cols;
     int slot = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const int64_t at = axis_offset_fast(a.row, row);
         const f32x4 st = *reinterpret_cast<const f32x4 *>(a.stats + 4 * row);
         float m[2] = {0.f, 0.f}, mp[2] = {0.f, 0.f};
-        if (a.pre_kind != CUBE3D_NORM_NONE) {
-            for (int c = threadIdx.x; c < a.cols; c += ROW_LANES) {
+        if (pre) {
+            for (int c = threadIdx.x * V; c < a.cols; c += ROW_LANES * V) {
                 const int64_t i = at + axis_offset_fast(a.col, c);
-                const float t = to_f32<TB>(dn[i]) * vector_at(a.p.pre_gamma, a.vec, c, 1.f), hat = (to_f32<TS>(r[i]) - st[2]) * st[3];
-                m[0] += t;
-                m[1] = fmaf(t, hat, m[1]);
+                float t[V], hat[V], gamma[V];
+                get<TB, V>(dn, i, t);
+                get<TS, V>(r, i, hat);
+                vector_at<V>(a.p.pre_gamma, axis_offset_fast(a.vec, c), 1.f, gamma);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    t[e] *= gamma[e];
+                    m[0] += t[e];
+                    m[1] = fmaf(t[e], (hat[e] - st[2]) * st[3], m[1]);
+                }
             }
             row_sum<2, ROW_LANES>(m, lds, slot);
             m[0] = a.pre_kind == CUBE3D_NORM_LAYER ? m[0] * inv : 0.f;
             m[1] *= inv;
         }
         if (a.post_kind != CUBE3D_NORM_NONE) {
-            for (int c = threadIdx.x; c < a.cols; c += ROW_LANES) {
+            for (int c = threadIdx.x * V; c < a.cols; c += ROW_LANES * V) {
                 const int64_t i = at + axis_offset_fast(a.col, c);
-                const ColumnParams p = column_params(a, c);
-                float g = dr ? to_f32<TS>(dr[i]) : 0.f;
-                if (a.pre_kind != CUBE3D_NORM_NONE)
-                    g += st[3] * (to_f32<TB>(dn[i]) * p.pre_gamma - m[0] - (to_f32<TS>(r[i]) - st[2]) * st[3] * m[1]);
-                const float t = a.scale * p.gate * g * p.post_gamma, hat = (to_f32<TB>(u[i]) - st[0]) * st[1];
-                mp[0] += t;
-                mp[1] = fmaf(t, hat, mp[1]);
+                ColumnParams<V> p;
+                p.look_up(a, c);
+                float g[V], t[V], hat[V], w[V];
+                if (dr) get<TS, V>(dr, i, g);
+                else
+#pragma unroll
+                    for (int e = 0; e < V; ++e) g[e] = 0.f;
+                if (pre) {
+                    get<TB, V>(dn, i, t);
+                    get<TS, V>(r, i, hat);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) g[e] += st[3] * (t[e] * p.pre_gamma[e] - m[0] - (hat[e] - st[2]) * st[3] * m[1]);
+                }
+                get<TB, V>(u, i, w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float tp = a.scale * p.gate[e] * g[e] * p.post_gamma[e];
+                    mp[0] += tp;
+                    mp[1] = fmaf(tp, (w[e] - st[0]) * st[1], mp[1]);
+                }
             }
             row_sum<2, ROW_LANES>(mp, lds, slot);
             mp[0] = a.post_kind == CUBE3D_NORM_LAYER ? mp[0] * inv : 0.f;
@@ -161,58 +218,84 @@ template <typename TS, typename TB> __global__ __launch_bounds__(ROW_LANES) void
     }
 }
 
-// Everything that remains is element-wise but for the column sums: a workgroup takes 64 columns of a group of rows, a lane
-// one column of every fourth row, and leaves partial sums [group][vector][column].
-constexpr int VECTORS = 5;      // post_gamma, post_beta, gate, pre_gamma, pre_beta
-template <typename TS, typename TB>
+// Everything that remains is element-wise but for the column sums: a workgroup takes 64 V columns of a group of rows, a lane V of
+// every fourth row, and leaves partial sums [group][vector][column].
+template <typename TS, typename TB, int V>
 __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a, const float *__restrict__ scalars, float *__restrict__ partials,
                                                                int rows_per_group)
 {
-    __shared__ float lds[4][VECTORS][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    __shared__ float lds[4][64 * V];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = (blockIdx.x * 64 + lane) * V;
     const bool live = c < a.cols;
-    const int64_t col = live ? axis_offset_fast(a.col, c) : 0;
-    const ColumnParams p = live ? column_params(a, c) : ColumnParams{0.f, 0.f, 0.f, 0.f};
+    const int64_t col = axis_offset_fast(a.col, live ? c : 0);
+    ColumnParams<V> p;
+    p.look_up(a, live ? c : 0);
     const TS *dr = static_cast<const TS *>(a.dr), *r = static_cast<const TS *>(a.x);
     const TB *dn = static_cast<const TB *>(a.dn), *u = static_cast<const TB *>(a.u);
     TS *dx = static_cast<TS *>(a.dx);
     TB *du = static_cast<TB *>(a.du);
     const bool pre = a.pre_kind != CUBE3D_NORM_NONE, post = a.post_kind != CUBE3D_NORM_NONE;
-    float sum[VECTORS] = {0.f, 0.f, 0.f, 0.f, 0.f};
+    float sum[VECTORS][V];
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[v][e] = 0.f;
     const int64_t first = (int64_t)blockIdx.y * rows_per_group, last = min(first + rows_per_group, a.rows);
     for (int64_t row = first + wave; row < last && live; row += 4) {
         const int64_t i = axis_offset_fast(a.row, row) + col;
         const f32x4 none = {0.f, 0.f, 0.f, 0.f};
         const f32x4 st = pre || post ? *reinterpret_cast<const f32x4 *>(a.stats + 4 * row) : none;
         const f32x4 m = pre || post ? *reinterpret_cast<const f32x4 *>(scalars + 4 * row) : none;
-        float g = dr ? to_f32<TS>(dr[i]) : 0.f;
-        if (pre) {
-            const float d = to_f32<TB>(dn[i]), hat = (to_f32<TS>(r[i]) - st[2]) * st[3];
-            sum[3] = fmaf(d, hat, sum[3]);
-            sum[4] += d;
-            g += st[3] * (d * p.pre_gamma - m[0] - hat * m[1]);
-        }
-        if (dx) dx[i] = from_f32<TS>(g);
-        g *= a.scale;
-        if (post) {
-            const float hat = (to_f32<TB>(u[i]) - st[0]) * st[1];
-            sum[2] = fmaf(g, hat * p.post_gamma + p.post_beta, sum[2]);
-            g *= p.gate;
-            sum[0] = fmaf(g, hat, sum[0]);
-            sum[1] += g;
-            g = st[1] * (g * p.post_gamma - m[2] - hat * m[3]);
-        } else {
-            if (a.read_u) sum[2] = fmaf(g, to_f32<TB>(u[i]), sum[2]);
-            g *= p.gate;
-        }
-        if (du) du[i] = from_f32<TB>(g);
-    }
+        float g[V], d[V], hat[V], w[V];
+        if (dr) get<TS, V>(dr, i, g);
+        else
 #pragma unroll
-    for (int v = 0; v < VECTORS; ++v) lds[wave][v][lane] = sum[v];
-    __syncthreads();
-    if (!a.sums || !live) return;
-    for (int v = wave; v < VECTORS; v += 4)
-        partials[((int64_t)blockIdx.y * VECTORS + v) * a.cols + c] = ((lds[0][v][lane] + lds[1][v][lane]) + lds[2][v][lane]) + lds[3][v][lane];
+            for (int e = 0; e < V; ++e) g[e] = 0.f;
+        if (pre) {
+            get<TB, V>(dn, i, d);
+            get<TS, V>(r, i, hat);
+        }
+        if (post || a.read_u) get<TB, V>(u, i, w);
+        if (pre) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                hat[e] = (hat[e] - st[2]) * st[3];
+                sum[3][e] = fmaf(d[e], hat[e], sum[3][e]);
+                sum[4][e] += d[e];
+                g[e] += st[3] * (d[e] * p.pre_gamma[e] - m[0] - hat[e] * m[1]);
+            }
+        }
+        if (dx) put<TS, V>(dx, i, g);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            g[e] *= a.scale;
+            if (post) {
+                w[e] = (w[e] - st[0]) * st[1];
+                sum[2][e] = fmaf(g[e], w[e] * p.post_gamma[e] + p.post_beta[e], sum[2][e]);
+                g[e] *= p.gate[e];
+                sum[0][e] = fmaf(g[e], w[e], sum[0][e]);
+                sum[1][e] += g[e];
+                g[e] = st[1] * (g[e] * p.post_gamma[e] - m[2] - w[e] * m[3]);
+            } else {
+                if (a.read_u) sum[2][e] = fmaf(g[e], w[e], sum[2][e]);
+                g[e] *= p.gate[e];
+            }
+        }
+        if (du) put<TB, V>(du, i, g);
+    }
+    if (!a.sums) return;
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v) {
+        if (v > 0) __syncthreads();
+#pragma unroll
+        for (int e = 0; e < V; ++e) lds[wave][e * 64 + lane] = sum[v][e];
+        __syncthreads();
+        for (int x = threadIdx.x; x < 64 * V; x += 256) {
+            const int at = x % V * 64 + x / V, column = blockIdx.x * 64 * V + x;
+            if (column < a.cols)
+                partials[((int64_t)blockIdx.y * VECTORS + v) * a.cols + column] = ((lds[0][at] + lds[1][at]) + lds[2][at]) + lds[3][at];
+        }
+    }
 }
 
 // The groups' partial sums of one vector, in ascending order, to its diagonal storage (zeros off the diagonal).  A workgroup takes
@@ -239,6 +322,7 @@ __global__ __launch_bounds__(64 * FINISH_WAVES) void norm_bwd_finish_kernel(cons
     const int per = (groups + FINISH_WAVES - 1) / FINISH_WAVES, lo = min(wave * per, groups), hi = min(lo + per, groups);
     float sum = 0.f;
     if (live)
+#pragma unroll 8
         for (int g = lo; g < hi; ++g) sum += partials[((int64_t)g * VECTORS + blockIdx.z) * a.cols + c];
     lds[wave][lane] = sum;
     __syncthreads();
@@ -249,12 +333,385 @@ __global__ __launch_bounds__(64 * FINISH_WAVES) void norm_bwd_finish_kernel(cons
     }
 }
 
+// ---- rows in registers ----------------------------------------------------------------------------------
+// Where eight consecutive columns lie side by side in every array (blocks and vector shards of a multiple of eight columns), a row is held
+// by `waves` wavefronts, eight columns times P a lane, and read once; short rows share a workgroup.  A lane keeps its columns from
+// row to row: offsets and parameters are looked up once, the backward pass's column sums grow in registers, and the next row is
+// on its way while the last one's sums are formed.
+//
+// What bounds it: HBM.  TB/s of necessary bytes, forward / backward, a copy of 1 GiB making 4.8: 32768 x 8192 bf16 5.0 / 5.1;
+// 8192 x 2048 (200 MB, in part from the Infinity Cache) 5.8 / 4.9; 16384 x 8192 with both norms and an fp32 stream 5.1 / 5.0; 16384 x 12288 5.6
+// / 3.0 (backward by the kernels above, which read everything but dr twice).  Row by row from memory, as above in single elements, the
+// first was 1.0 / 1.7.
+
+constexpr int SHORT_ROW = 512;          // columns of one wavefront
+
+// Sum over the 64 lanes, in all of them, in a fixed order: within 16 lanes by exchanges inside the vector unit, then over the four rows.
+__device__ __forceinline__ float lanes16_sum(float x)
+{
+    auto moved = [](float v, auto ctrl) {
+        return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    x += moved(x, std::integral_constant<int, 0xb1>{});       // neighbours
+    x += moved(x, std::integral_constant<int, 0x4e>{});       // pairs
+    x += moved(x, std::integral_constant<int, 0x141>{});      // mirrored in eights
+    x += moved(x, std::integral_constant<int, 0x140>{});      // mirrored in sixteens
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x)
+{
+    x = lanes16_sum(x);
+    const int i = (int)__float_as_uint(x);
+    const float a = __uint_as_float((unsigned)__builtin_amdgcn_readlane(i, 0)), b = __uint_as_float((unsigned)__builtin_amdgcn_readlane(i, 16));
+    const float c = __uint_as_float((unsigned)__builtin_amdgcn_readlane(i, 32)), d = __uint_as_float((unsigned)__builtin_amdgcn_readlane(i, 48));
+    return (a + b) + (c + d);
+}
+
+// The wavefronts of one row: `waves` (at most 16) of them, the first of which is number `first` of the workgroup.
+struct RowGroup {
+    int waves, first, wave, lane;
+    float (*lds)[2][16];        // [slot][value][wavefront], for the whole workgroup
+    int slot;
+};
+
+// Sums of K values over a row, in all its lanes.  (All wavefronts of the workgroup call it together.)
+template <int K> __device__ __forceinline__ void group_sum(RowGroup &g, float (&x)[K])
+{
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = wave_sum(x[k]);
+    if (g.waves == 1) return;
+    g.slot ^= 1;        // (read until the next call's barrier, overwritten behind it)
+    if (g.lane == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k) g.lds[g.slot][k][g.wave] = x[k];
+    __syncthreads();
+    const int l = g.lane % 16;
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = lanes16_sum(l < g.waves ? g.lds[g.slot][k][(g.first + l) % 16] : 0.f);
+}
+
+template <typename T> __device__ __forceinline__ void unpack(const Pack8<T> &v, float (&x)[VEC])
+{
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = to_f32<T>(v.v[e]);
+}
+
+template <typename TS, typename TB, int P> __global__ __launch_bounds__(1024) void norm_fwd_kernel(const NormArgs a, int waves, int rows_at_once)
+{
+    __shared__ float lds[2][2][16];
+    RowGroup g;
+    g.lane = threadIdx.x % 64;
+    g.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    g.waves = waves;
+    const int group = g.wave / waves;
+    g.first = group * waves;
+    g.lds = lds;
+    g.slot = 0;
+    const TS *x = static_cast<const TS *>(a.x);
+    const TB *u = static_cast<const TB *>(a.u);
+    TS *r_out = static_cast<TS *>(a.r_out);
+    TB *n_out = static_cast<TB *>(a.n_out);
+    const bool post = a.post_kind != CUBE3D_NORM_NONE, pre = a.pre_kind != CUBE3D_NORM_NONE;
+    const float inv = 1.f / (float)a.cols;
+    int64_t col[P];
+    bool live[P];
+    // (two pieces a lane leave no registers for the parameters: those are read row by row)
+    constexpr bool HELD = P == 1;
+    float post_gamma[VEC], post_beta[VEC], gate[VEC], pre_gamma[VEC], pre_beta[VEC];
+    int64_t vec[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const int c = ((p * waves + g.wave - g.first) * 64 + g.lane) * VEC;
+        live[p] = c < a.cols;
+        const int cc = live[p] ? c : 0;
+        col[p] = axis_offset_fast(a.col, cc);
+        vec[p] = axis_offset_fast(a.vec, cc);
+    }
+    auto look_up_post = [&](int p) {
+        vector_at<VEC>(a.p.post_gamma, vec[p], 1.f, post_gamma);
+        vector_at<VEC>(a.p.post_beta, vec[p], 0.f, post_beta);
+    };
+    auto look_up_gate = [&](int p) { vector_at<VEC>(a.p.gate, vec[p], 1.f, gate); };
+    auto look_up_pre = [&](int p) {
+        vector_at<VEC>(a.p.pre_gamma, vec[p], 1.f, pre_gamma);
+        vector_at<VEC>(a.p.pre_beta, vec[p], 0.f, pre_beta);
+    };
+    if constexpr (HELD) {
+        look_up_post(0);
+        look_up_gate(0);
+        look_up_pre(0);
+    }
+    Pack8<TS> xr[P];
+    Pack8<TB> ur[P];
+    const int64_t step = (int64_t)gridDim.x * rows_at_once;
+    auto load = [&](int64_t row) {
+        const int64_t at = axis_offset_fast(a.row, min(row, a.rows - 1));
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            xr[p] = *reinterpret_cast<const Pack8<TS> *>(x + at + col[p]);
+            if (a.u) ur[p] = *reinterpret_cast<const Pack8<TB> *>(u + at + col[p]);
+        }
+    };
+    // sum over the row of f(piece, element), lanes beyond its end aside
+    auto total = [&](auto &&f) {
+        float s[1] = {0.f};
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) s[0] += live[p] ? f(p, e) : 0.f;
+        group_sum<1>(g, s);
+        return s[0];
+    };
+    int64_t row = (int64_t)blockIdx.x * rows_at_once + group;
+    load(row);
+    // (all wavefronts of the workgroup take as many turns: row_sum has barriers)
+    for (int64_t base = (int64_t)blockIdx.x * rows_at_once; base < a.rows; base += step, row += step) {
+        float r[P][VEC], v[P][VEC];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            unpack(xr[p], r[p]);
+            if (a.u) unpack(ur[p], v[p]);
+        }
+        if (base + step < a.rows) load(row + step);
+        float post_mean = 0.f, post_rstd = 0.f, pre_mean = 0.f, pre_rstd = 0.f;
+        if (post) {
+            if (a.post_kind == CUBE3D_NORM_LAYER) post_mean = total([&](int p, int e) { return v[p][e]; }) * inv;
+            const float var = total([&](int p, int e) { return (v[p][e] - post_mean) * (v[p][e] - post_mean); }) * inv;
+            post_rstd = 1.f / sqrtf(var + a.post_eps);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if constexpr (!HELD) look_up_post(p);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[p][e] = (v[p][e] - post_mean) * post_rstd * post_gamma[e] + post_beta[e];
+            }
+        }
+        if (a.u) {
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                if constexpr (!HELD) look_up_gate(p);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) r[p][e] += a.scale * gate[e] * v[p][e];
+            }
+        }
+        if (pre) {
+            if (a.pre_kind == CUBE3D_NORM_LAYER) pre_mean = total([&](int p, int e) { return r[p][e]; }) * inv;
+            const float var = total([&](int p, int e) { return (r[p][e] - pre_mean) * (r[p][e] - pre_mean); }) * inv;
+            pre_rstd = 1.f / sqrtf(var + a.pre_eps);
+        }
+        if (row >= a.rows) continue;
+        const int64_t at = axis_offset_fast(a.row, row);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if (!live[p]) continue;
+            if (r_out) *reinterpret_cast<Pack8<TS> *>(r_out + at + col[p]) = pack_out<TS>(r[p]);
+            if (pre) {
+                if constexpr (!HELD) look_up_pre(p);
+                float n[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) n[e] = (r[p][e] - pre_mean) * pre_rstd * pre_gamma[e] + pre_beta[e];
+                *reinterpret_cast<Pack8<TB> *>(n_out + at + col[p]) = pack_out<TB>(n);
+            }
+        }
+        if (a.stats_out && g.wave == g.first && g.lane == 0)
+            *reinterpret_cast<f32x4 *>(a.stats_out + 4 * row) = f32x4{post_mean, post_rstd, pre_mean, pre_rstd};
+    }
+}
+
+// Workgroup w leaves the sums over its rows in partials[w].  MOST: wavefronts of a workgroup.  Both norms at once take some 160
+// registers a lane: eight wavefronts then (2997 x 1152 20.7 us for 45 with sixteen, which spill); where a row needs sixteen the
+// parameters are read row by row and no row ahead (16384 x 8192 482 us for 726).
+template <typename TS, typename TB, bool PRE, bool POST, int MOST>
+__global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, float *__restrict__ partials, int waves, int rows_at_once)
+{
+    __shared__ float lds[2][2][16];
+    extern __shared__ float tail[];      // rows_at_once > 1: their column sums, one vector at a time
+    RowGroup g;
+    g.lane = threadIdx.x % 64;
+    g.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    g.waves = waves;
+    const int group = g.wave / waves;
+    g.first = group * waves;
+    g.lds = lds;
+    g.slot = 0;
+    const TS *dr = static_cast<const TS *>(a.dr), *r = static_cast<const TS *>(a.x);
+    const TB *dn = static_cast<const TB *>(a.dn), *u = static_cast<const TB *>(a.u);
+    TS *dx = static_cast<TS *>(a.dx);
+    TB *du = static_cast<TB *>(a.du);
+    const float inv = 1.f / (float)a.cols;
+    const int own = (g.wave - g.first) * 64 + g.lane, c = own * VEC;
+    const bool live = c < a.cols;
+    const int64_t col = axis_offset_fast(a.col, live ? c : 0), vec = axis_offset_fast(a.vec, live ? c : 0);
+    float post_gamma[VEC], post_beta[VEC], gate[VEC], pre_gamma[VEC];
+    constexpr bool HELD = !(PRE && POST && MOST == 16);
+    auto look_up_pre = [&]() { vector_at<VEC>(a.p.pre_gamma, vec, 1.f, pre_gamma); };
+    auto look_up_post = [&]() {
+        vector_at<VEC>(a.p.gate, vec, 1.f, gate);
+        if constexpr (POST) {
+            vector_at<VEC>(a.p.post_gamma, vec, 1.f, post_gamma);
+            vector_at<VEC>(a.p.post_beta, vec, 0.f, post_beta);
+        }
+    };
+    if constexpr (HELD) {
+        if constexpr (PRE) look_up_pre();
+        look_up_post();
+    }
+    float sum[VECTORS][VEC];
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[v][e] = 0.f;
+    Pack8<TS> dr_raw, r_raw;
+    Pack8<TB> dn_raw, u_raw;
+    f32x4 st_raw;
+    const bool with_u = POST || a.read_u;
+    auto load = [&](int64_t row) {
+        const int64_t rr = min(row, a.rows - 1), at = axis_offset_fast(a.row, rr) + col;
+        if (dr) dr_raw = *reinterpret_cast<const Pack8<TS> *>(dr + at);
+        if constexpr (PRE) {
+            dn_raw = *reinterpret_cast<const Pack8<TB> *>(dn + at);
+            r_raw = *reinterpret_cast<const Pack8<TS> *>(r + at);
+        }
+        if (with_u) u_raw = *reinterpret_cast<const Pack8<TB> *>(u + at);
+        if constexpr (PRE || POST) st_raw = *reinterpret_cast<const f32x4 *>(a.stats + 4 * rr);
+    };
+    const int64_t step = (int64_t)gridDim.x * rows_at_once;
+    int64_t row = (int64_t)blockIdx.x * rows_at_once + group;
+    load(row);
+    for (int64_t base = (int64_t)blockIdx.x * rows_at_once; base < a.rows; base += step, row += step) {
+        const bool here = live && row < a.rows;
+        float d[VEC], t[VEC], hat[VEC], w[VEC];
+        f32x4 st;
+        if (dr) unpack(dr_raw, d);
+        else
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) d[e] = 0.f;
+        if constexpr (PRE) {
+            unpack(dn_raw, t);
+            unpack(r_raw, hat);
+        }
+        if (with_u) unpack(u_raw, w);
+        if constexpr (PRE || POST) st = st_raw;
+        const int64_t at = axis_offset_fast(a.row, min(row, a.rows - 1)) + col;
+        if (HELD && base + step < a.rows) load(row + step);
+        if constexpr (PRE) {
+            if constexpr (!HELD) look_up_pre();
+            float m[2] = {0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                hat[e] = (hat[e] - st[2]) * st[3];
+                const float b = here ? t[e] : 0.f;
+                sum[3][e] = fmaf(b, here ? hat[e] : 0.f, sum[3][e]);
+                sum[4][e] += b;
+                t[e] = here ? t[e] * pre_gamma[e] : 0.f;
+                m[0] += t[e];
+                m[1] = fmaf(t[e], here ? hat[e] : 0.f, m[1]);
+            }
+            group_sum<2>(g, m);
+            const float m0 = a.pre_kind == CUBE3D_NORM_LAYER ? m[0] * inv : 0.f, m1 = m[1] * inv;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) d[e] += st[3] * (t[e] - m0 - hat[e] * m1);
+        }
+        if (dx && here) *reinterpret_cast<Pack8<TS> *>(dx + at) = pack_out<TS>(d);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) d[e] = here ? d[e] * a.scale : 0.f;
+        if constexpr (!HELD) look_up_post();
+        if constexpr (POST) {
+            float m[2] = {0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                w[e] = here ? (w[e] - st[0]) * st[1] : 0.f;
+                sum[2][e] = fmaf(d[e], w[e] * post_gamma[e] + post_beta[e], sum[2][e]);
+                d[e] *= gate[e];
+                sum[0][e] = fmaf(d[e], w[e], sum[0][e]);
+                sum[1][e] += d[e];
+                d[e] *= post_gamma[e];
+                m[0] += d[e];
+                m[1] = fmaf(d[e], w[e], m[1]);
+            }
+            group_sum<2>(g, m);
+            const float m0 = a.post_kind == CUBE3D_NORM_LAYER ? m[0] * inv : 0.f, m1 = m[1] * inv;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) d[e] = st[1] * (d[e] - m0 - w[e] * m1);
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                if (with_u) sum[2][e] = fmaf(d[e], here ? w[e] : 0.f, sum[2][e]);
+                d[e] *= gate[e];
+            }
+        }
+        if (du && here) *reinterpret_cast<Pack8<TB> *>(du + at) = pack_out<TB>(d);
+        if (!HELD && base + step < a.rows) load(row + step);
+    }
+    if (!a.sums) return;
+    float *out = partials + (int64_t)blockIdx.x * VECTORS * a.cols;
+    const int width = waves * 64 * VEC;
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v) {
+        if (v < 2 && !POST) continue;
+        if (v > 2 && !PRE) continue;
+        if (rows_at_once > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) tail[group * width + e * waves * 64 + own] = sum[v][e];
+            __syncthreads();
+            if (group == 0)
+                for (int k = 1; k < rows_at_once; ++k)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sum[v][e] += tail[k * width + e * waves * 64 + own];
+        }
+        if (group == 0 && live) {
+            f32x4 *dst = reinterpret_cast<f32x4 *>(out + (int64_t)v * a.cols + c);
+            dst[0] = f32x4{sum[v][0], sum[v][1], sum[v][2], sum[v][3]};
+            dst[1] = f32x4{sum[v][4], sum[v][5], sum[v][6], sum[v][7]};
+        }
+    }
+}
+
+bool eights(const NormArgs &a)
+{
+    for (const AxisMap *m : {&a.col, &a.vec})
+        if (m->P1 % VEC || m->P2 % VEC || m->s1 % VEC || m->s2 % VEC) return false;
+    return a.row.u % VEC == 0 && a.row.s1 % VEC == 0 && a.row.s2 % VEC == 0 && a.cols % VEC == 0;
+}
+
+// How rows are dealt out: wavefronts per row, rows per workgroup, pieces of eight columns per lane, workgroups; waves = 0: the row does not
+// fit, or does not lie in eights.
+struct RowPlan {
+    int waves, rows_at_once, pieces;
+    unsigned groups;
+};
+
+RowPlan row_plan(const NormArgs &a, bool backward)
+{
+    RowPlan p{0, 1, 1, 0};
+    if (!eights(a)) return p;
+    const int most = backward ? 16 * SHORT_ROW : 32 * SHORT_ROW;
+    if (a.cols > most) return p;
+    p.pieces = !backward && a.cols > 16 * SHORT_ROW ? 2 : 1;
+    p.waves = (a.cols + SHORT_ROW * p.pieces - 1) / (SHORT_ROW * p.pieces);
+    const int64_t cus = num_compute_units();
+    if (backward) {
+        // A workgroup leaves a partial sum of every vector: as few of them as fill the CUs, of as many rows at once as that allows
+        // (2997 rows of 1152 with one norm, 62 MB: 45 us with 5 rows at once, 65 with one on five times as many workgroups)
+        const bool both = a.pre_kind != CUBE3D_NORM_NONE && a.post_kind != CUBE3D_NORM_NONE;
+        const int fit = (both && p.waves <= 8 ? 8 : 16) / p.waves;
+        const int64_t each = (a.rows + cus - 1) / cus;
+        p.rows_at_once = fit < each ? fit : (int)each;
+    } else p.rows_at_once = p.waves == 1 ? 4 : p.waves == 2 ? 2 : 1;
+    // about sixteen wavefronts a CU
+    const int64_t per_cu = backward || p.waves * p.rows_at_once > 16 ? 1 : 16 / (p.waves * p.rows_at_once);
+    int64_t groups = (a.rows + p.rows_at_once - 1) / p.rows_at_once;
+    if (groups > cus * per_cu) groups = cus * per_cu;
+    p.groups = (unsigned)groups;
+    return p;
+}
+
 // Rows per workgroup of the column pass: enough workgroups for every CU, few enough partial sums.
 int rows_per_group(const NormArgs &a)
 {
-    const int64_t tiles = (a.cols + 63) / 64;
+    const int64_t width = eights(a) ? 64 * VEC : 64, tiles = (a.cols + width - 1) / width;
     int64_t rows = 256;
-    while (rows > 16 && tiles * ((a.rows + rows - 1) / rows) < 4096) rows /= 2;
+    while (rows > 16 && tiles * ((a.rows + rows - 1) / rows) < 2048) rows /= 2;
     while ((a.rows + rows - 1) / rows > 32768) rows *= 2;
     return (int)rows;
 }
@@ -276,38 +733,86 @@ unsigned row_grid(int64_t rows)
 
 int norm_fwd(const NormArgs &a, hipStream_t stream)
 {
+    const RowPlan plan = row_plan(a, false);
     return by_types(a, [&](auto s, auto b) {
-        hipLaunchKernelGGL((norm_fwd_rows_kernel<decltype(s), decltype(b)>), dim3(row_grid(a.rows)), dim3(ROW_LANES), 0, stream, a);
+        typedef decltype(s) TS;
+        typedef decltype(b) TB;
+        const dim3 block(64 * plan.waves * plan.rows_at_once);
+        if (plan.waves == 0 && eights(a))
+            hipLaunchKernelGGL((norm_fwd_rows_kernel<TS, TB, VEC>), dim3(row_grid(a.rows)), dim3(ROW_LANES), 0, stream, a);
+        else if (plan.waves == 0)
+            hipLaunchKernelGGL((norm_fwd_rows_kernel<TS, TB, 1>), dim3(row_grid(a.rows)), dim3(ROW_LANES), 0, stream, a);
+        else if (plan.pieces == 1)
+            hipLaunchKernelGGL((norm_fwd_kernel<TS, TB, 1>), dim3(plan.groups), block, 0, stream, a, plan.waves, plan.rows_at_once);
+        else
+            hipLaunchKernelGGL((norm_fwd_kernel<TS, TB, 2>), dim3(plan.groups), block, 0, stream, a, plan.waves, plan.rows_at_once);
         return launch_status();
     });
 }
 
 size_t norm_bwd_workspace(const NormArgs &a)
 {
+    const RowPlan plan = row_plan(a, true);
+    if (plan.waves > 0) return (size_t)plan.groups * VECTORS * a.cols * sizeof(float);
     const int64_t per = rows_per_group(a), groups = (a.rows + per - 1) / per;
     return ((size_t)a.rows * 4 + (size_t)groups * VECTORS * a.cols) * sizeof(float);
 }
 
+namespace {
+
+int finish(const NormArgs &a, const float *partials, unsigned groups, const cube3d_norm_params &gradients, hipStream_t stream)
+{
+    const unsigned q3 = (unsigned)(a.q * a.q * a.q);
+    hipLaunchKernelGGL(norm_bwd_finish_kernel, dim3((unsigned)((a.vec.P2 + 63) / 64), q3, VECTORS), dim3(64 * FINISH_WAVES), 0, stream, a,
+                       partials, (int)groups, gradients);
+    return launch_status();
+}
+
+}  // namespace
+
 int norm_bwd(const NormArgs &a, const cube3d_norm_params &gradients, void *workspace, hipStream_t stream)
 {
+    const bool pre = a.pre_kind != CUBE3D_NORM_NONE, post = a.post_kind != CUBE3D_NORM_NONE;
+    if (const RowPlan plan = row_plan(a, true); plan.waves > 0) {
+        float *partials = static_cast<float *>(workspace);
+        const dim3 grid(plan.groups), block(64 * plan.waves * plan.rows_at_once);
+        const size_t lds = plan.rows_at_once > 1 ? sizeof(float) * plan.rows_at_once * plan.waves * SHORT_ROW : 0;
+        const int rc = by_types(a, [&](auto s, auto b) {
+            typedef decltype(s) TS;
+            typedef decltype(b) TB;
+            auto launch = [&](auto pre_c, auto post_c) {
+                constexpr bool PRE = decltype(pre_c)::value, POST = decltype(post_c)::value;
+                if (PRE && POST && plan.waves <= 8)
+                    hipLaunchKernelGGL((norm_bwd_kernel<TS, TB, PRE, POST, PRE && POST ? 8 : 16>), grid, block, lds, stream, a, partials,
+                                       plan.waves, plan.rows_at_once);
+                else
+                    hipLaunchKernelGGL((norm_bwd_kernel<TS, TB, PRE, POST, 16>), grid, block, lds, stream, a, partials, plan.waves,
+                                       plan.rows_at_once);
+                return launch_status();
+            };
+            const std::true_type yes{};
+            const std::false_type no{};
+            return pre ? (post ? launch(yes, yes) : launch(yes, no)) : (post ? launch(no, yes) : launch(no, no));
+        });
+        return rc != CUBE3D_OK || !a.sums ? rc : finish(a, partials, plan.groups, gradients, stream);
+    }
     float *scalars = static_cast<float *>(workspace), *partials = scalars + a.rows * 4;
     const int per = rows_per_group(a);
     const unsigned groups = (unsigned)((a.rows + per - 1) / per);
     const int rc = by_types(a, [&](auto s, auto b) {
         typedef decltype(s) TS;
         typedef decltype(b) TB;
-        if (a.pre_kind != CUBE3D_NORM_NONE || a.post_kind != CUBE3D_NORM_NONE)
-            hipLaunchKernelGGL((norm_bwd_rows_kernel<TS, TB>), dim3(row_grid(a.rows)), dim3(ROW_LANES), 0, stream, a, scalars);
-        if (const int e = launch_status(); e != CUBE3D_OK) return e;
-        hipLaunchKernelGGL((norm_bwd_columns_kernel<TS, TB>), dim3((unsigned)((a.cols + 63) / 64), groups), dim3(256), 0, stream, a,
-                           scalars, partials, per);
-        return launch_status();
+        auto launch = [&](auto v) {
+            constexpr int V = decltype(v)::value;
+            if (pre || post) hipLaunchKernelGGL((norm_bwd_rows_kernel<TS, TB, V>), dim3(row_grid(a.rows)), dim3(ROW_LANES), 0, stream, a, scalars);
+            if (const int e = launch_status(); e != CUBE3D_OK) return e;
+            hipLaunchKernelGGL((norm_bwd_columns_kernel<TS, TB, V>), dim3((unsigned)((a.cols + 64 * V - 1) / (64 * V)), groups), dim3(256), 0,
+                               stream, a, scalars, partials, per);
+            return launch_status();
+        };
+        return eights(a) ? launch(std::integral_constant<int, VEC>{}) : launch(std::integral_constant<int, 1>{});
     });
-    if (rc != CUBE3D_OK || !a.sums) return rc;
-    const unsigned q3 = (unsigned)(a.q * a.q * a.q);
-    hipLaunchKernelGGL(norm_bwd_finish_kernel, dim3((unsigned)((a.vec.P2 + 63) / 64), q3, VECTORS), dim3(64 * FINISH_WAVES), 0, stream, a,
-                       partials, (int)groups, gradients);
-    return launch_status();
+    return rc != CUBE3D_OK || !a.sums ? rc : finish(a, partials, groups, gradients, stream);
 }
 
 }  // namespace cube3d

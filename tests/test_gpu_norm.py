@@ -172,6 +172,19 @@ def test_sizes(q, axis, rows, cols, stream, blk, post, pre):
     check_backward(pr)
 
 
+# many turns of every workgroup, rows shared by a workgroup with a last turn that is not full, and rows too long for registers
+MANY = [(1, "y", 20011, 8), (1, "z", 9001, 512), (2, "y", 6004, 520), (1, "y", 2600, 2048), (3, "z", 2997, 1152), (1, "y", 700, 8192), (2, "z", 600, 4608),
+        (1, "y", 300, 9216), (1, "z", 9, 24576), (1, "y", 40, 16640)]
+
+
+@pytest.mark.parametrize("q,axis,rows,cols", MANY)
+@pytest.mark.parametrize("post,pre", [("layer", "layer"), ("none", "rms"), ("rms", "none")])
+def test_many_rows_and_long_ones(q, axis, rows, cols, post, pre):
+    pr = Problem(q, axis, rows, cols, "f32" if post == "layer" else "bf16", "bf16", post, pre)
+    check_forward(pr, *pr.forward())
+    check_backward(pr)
+
+
 @pytest.mark.parametrize("cols", [256, 129, 9000])
 def test_optional_parts(cols):
     """No parameters; no block (a norm alone); no residual gradient; single results; in place."""
