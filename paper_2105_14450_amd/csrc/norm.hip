@@ -18,7 +18,10 @@ namespace {
 constexpr int VECTORS = 5;      // post_gamma, post_beta, gate, pre_gamma, pre_beta
 
 // ---- any size: one workgroup per row, the row read again for every step ---------------------------------
-// V consecutive columns at a time: eight where they lie side by side in every array, else one.
+// V consecutive columns at a time: eight where they lie side by side in every array, else four, two or one.  Bound by the
+// latency of narrow loads and of the passes over a row, of which a forward pass makes up to four: us, forward / backward,
+// 3000 x 4100 (four) 31 / 51, 20000 x 514 (two) 47 / 56, 3000 x 4101 (one) 68 / 85; in single elements the first was 69 / 84, the
+// second 94 / 97 (with four wavefronts a row).
 
 constexpr int ROW_LANES = 256;
 
@@ -70,9 +73,9 @@ template <int V> __device__ __forceinline__ void vector_at(const float *v, int64
         for (int e = 0; e < V; ++e) x[e] = absent;
 }
 
-template <typename TS, typename TB, int V> __global__ __launch_bounds__(ROW_LANES) void norm_fwd_rows_kernel(const NormArgs a)
+template <typename TS, typename TB, int V, int LANES> __global__ __launch_bounds__(LANES) void norm_fwd_rows_kernel(const NormArgs a)
 {
-    __shared__ float lds[2][ROW_LANES / 64 * 4];
+    __shared__ float lds[2][LANES / 64 * 4];
     const TS *x = static_cast<const TS *>(a.x);
     const TB *u = static_cast<const TB *>(a.u);
     TS *r = static_cast<TS *>(a.r_out);
@@ -85,13 +88,13 @@ template <typename TS, typename TB, int V> __global__ __launch_bounds__(ROW_LANE
         // sum over the row of f(value), f of V columns at a time
         auto total = [&](auto &&values, auto &&f) {
             float s[1] = {0.f};
-            for (int c = threadIdx.x * V; c < a.cols; c += ROW_LANES * V) {
+            for (int c = threadIdx.x * V; c < a.cols; c += LANES * V) {
                 float v[V];
                 values(c, at + axis_offset_fast(a.col, c), v);
 #pragma unroll
                 for (int e = 0; e < V; ++e) s[0] += f(v[e]);
             }
-            row_sum<1, ROW_LANES>(s, lds, slot);
+            row_sum<1, LANES>(s, lds, slot);
             return s[0];
         };
         if (a.post_kind != CUBE3D_NORM_NONE) {
@@ -121,7 +124,7 @@ template <typename TS, typename TB, int V> __global__ __launch_bounds__(ROW_LANE
             if (a.pre_kind == CUBE3D_NORM_LAYER) pre_mean = total(stream, [](float v) { return v; }) * inv;
             pre_rstd = 1.f / sqrtf(total(stream, [&](float v) { return (v - pre_mean) * (v - pre_mean); }) * inv + a.pre_eps);
         }
-        for (int c = threadIdx.x * V; c < a.cols; c += ROW_LANES * V) {
+        for (int c = threadIdx.x * V; c < a.cols; c += LANES * V) {
             const int64_t i = at + axis_offset_fast(a.col, c);
             float v[V];
             stream(c, i, v);
@@ -155,10 +158,10 @@ template <int V> struct ColumnParams {
 };
 
 // Row sums of the backward pass: scalars[row] = mean(t), mean(t r^), mean(tp), mean(tp u^)
-template <typename TS, typename TB, int V>
-__global__ __launch_bounds__(ROW_LANES) void norm_bwd_rows_kernel(const NormArgs a, float *__restrict__ scalars)
+template <typename TS, typename TB, int V, int LANES>
+__global__ __launch_bounds__(LANES) void norm_bwd_rows_kernel(const NormArgs a, float *__restrict__ scalars)
 {
-    __shared__ float lds[2][ROW_LANES / 64 * 4];
+    __shared__ float lds[2][LANES / 64 * 4];
     const TS *dr = static_cast<const TS *>(a.dr), *r = static_cast<const TS *>(a.x);
     const TB *dn = static_cast<const TB *>(a.dn), *u = static_cast<const TB *>(a.u);
     const bool pre = a.pre_kind != CUBE3D_NORM_NONE;
@@ -169,7 +172,7 @@ __global__ __launch_bounds__(ROW_LANES) void norm_bwd_rows_kernel(const NormArgs
         const f32x4 st = *reinterpret_cast<const f32x4 *>(a.stats + 4 * row);
         float m[2] = {0.f, 0.f}, mp[2] = {0.f, 0.f};
         if (pre) {
-            for (int c = threadIdx.x * V; c < a.cols; c += ROW_LANES * V) {
+            for (int c = threadIdx.x * V; c < a.cols; c += LANES * V) {
                 const int64_t i = at + axis_offset_fast(a.col, c);
                 float t[V], hat[V], gamma[V];
                 get<TB, V>(dn, i, t);
@@ -182,12 +185,12 @@ __global__ __launch_bounds__(ROW_LANES) void norm_bwd_rows_kernel(const NormArgs
                     m[1] = fmaf(t[e], (hat[e] - st[2]) * st[3], m[1]);
                 }
             }
-            row_sum<2, ROW_LANES>(m, lds, slot);
+            row_sum<2, LANES>(m, lds, slot);
             m[0] = a.pre_kind == CUBE3D_NORM_LAYER ? m[0] * inv : 0.f;
             m[1] *= inv;
         }
         if (a.post_kind != CUBE3D_NORM_NONE) {
-            for (int c = threadIdx.x * V; c < a.cols; c += ROW_LANES * V) {
+            for (int c = threadIdx.x * V; c < a.cols; c += LANES * V) {
                 const int64_t i = at + axis_offset_fast(a.col, c);
                 ColumnParams<V> p;
                 p.look_up(a, c);
@@ -210,7 +213,7 @@ __global__ __launch_bounds__(ROW_LANES) void norm_bwd_rows_kernel(const NormArgs
                     mp[1] = fmaf(tp, (w[e] - st[0]) * st[1], mp[1]);
                 }
             }
-            row_sum<2, ROW_LANES>(mp, lds, slot);
+            row_sum<2, LANES>(mp, lds, slot);
             mp[0] = a.post_kind == CUBE3D_NORM_LAYER ? mp[0] * inv : 0.f;
             mp[1] *= inv;
         }
@@ -340,9 +343,8 @@ __global__ __launch_bounds__(64 * FINISH_WAVES) void norm_bwd_finish_kernel(cons
 // on its way while the last one's sums are formed.
 //
 // What bounds it: HBM.  TB/s of necessary bytes, forward / backward, a copy of 1 GiB making 4.8: 32768 x 8192 bf16 5.0 / 5.1;
-// 8192 x 2048 (200 MB, in part from the Infinity Cache) 5.8 / 4.9; 16384 x 8192 with both norms and an fp32 stream 5.1 / 5.0; 16384 x 12288 5.6
-// / 3.0 (backward by the kernels above, which read everything but dr twice).  Row by row from memory, as above in single elements, the
-// first was 1.0 / 1.7.
+// 8192 x 2048 (200 MB, in part from the Infinity Cache) 5.8 / 4.9; 16384 x 8192 with both norms and an fp32 stream 5.1 / 5.0;
+// 16384 x 12288 5.6 / 5.0 (norm_bwd_long_kernel).  Row by row from memory, as above in single elements, the first was 1.0 / 1.7.
 
 constexpr int SHORT_ROW = 512;          // columns of one wavefront
 
@@ -667,11 +669,175 @@ __global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, f
     }
 }
 
-bool eights(const NormArgs &a)
+// Consecutive columns that lie side by side and aligned in every array: eight, four, two or one
+int widest(const NormArgs &a)
 {
-    for (const AxisMap *m : {&a.col, &a.vec})
-        if (m->P1 % VEC || m->P2 % VEC || m->s1 % VEC || m->s2 % VEC) return false;
-    return a.row.u % VEC == 0 && a.row.s1 % VEC == 0 && a.row.s2 % VEC == 0 && a.cols % VEC == 0;
+    for (int v : {VEC, VEC / 2, VEC / 4}) {
+        bool fits = a.row.u % v == 0 && a.row.s1 % v == 0 && a.row.s2 % v == 0 && a.cols % v == 0;
+        for (const AxisMap *m : {&a.col, &a.vec}) fits = fits && m->P1 % v == 0 && m->P2 % v == 0 && m->s1 % v == 0 && m->s2 % v == 0;
+        if (fits) return v;
+    }
+    return 1;
+}
+
+template <typename F> int by_width(const NormArgs &a, F &&f)
+{
+    switch (widest(a)) {
+    case VEC: return f(std::integral_constant<int, VEC>{});
+    case VEC / 2: return f(std::integral_constant<int, VEC / 2>{});
+    case VEC / 4: return f(std::integral_constant<int, VEC / 4>{});
+    default: return f(std::integral_constant<int, 1>{});
+    }
+}
+
+// Rows of up to 16384 columns, sixteen a lane: the registers hold a row and nothing else, so the parameters are read row by row and the
+// column sums lie in LDS, where a lane finds its own (16 columns x 1024 lanes x 4 bytes for each vector asked for).  Where the vectors
+// asked for do not fit, the two passes for any size take the call.  us, here / there: 16384 x 12288 bf16 402 / 668,
+// 8192 x 16384 271 / 473, 16384 x 12288 with an fp32 stream and both norms 741 / 1300.
+constexpr int LONG_SUMS = 38400;         // floats: 150 KB of the 160
+template <typename TS, typename TB, bool PRE, bool POST>
+__global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormArgs a, float *__restrict__ partials, int waves, int wanted)
+{
+    constexpr int P = 2;
+    __shared__ float lds[2][2][16];
+    __shared__ __attribute__((aligned(16))) float sums[LONG_SUMS];
+    RowGroup g;
+    g.lane = threadIdx.x % 64;
+    g.wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    g.waves = waves;
+    g.first = 0;
+    g.lds = lds;
+    g.slot = 0;
+    const TS *dr = static_cast<const TS *>(a.dr), *r = static_cast<const TS *>(a.x);
+    const TB *dn = static_cast<const TB *>(a.dn), *u = static_cast<const TB *>(a.u);
+    TS *dx = static_cast<TS *>(a.dx);
+    TB *du = static_cast<TB *>(a.du);
+    const float inv = 1.f / (float)a.cols;
+    const int lanes = waves * 64;
+    int64_t col[P], vec[P];
+    bool live[P];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+        const int c = (p * lanes + (int)threadIdx.x) * VEC;
+        live[p] = c < a.cols;
+        col[p] = axis_offset_fast(a.col, live[p] ? c : 0);
+        vec[p] = axis_offset_fast(a.vec, live[p] ? c : 0);
+    }
+    // a lane's eight sums of vector v (the n-th of the wanted ones), piece p
+    auto place = [&](int v, int p, int half) {
+        const int n = __builtin_popcount(wanted & ((1 << v) - 1));
+        return reinterpret_cast<f32x4 *>(sums) + ((n * P + p) * 2 + half) * lanes + threadIdx.x;
+    };
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v)
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (wanted >> v & 1) *place(v, p, 0) = *place(v, p, 1) = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto add = [&](int v, int p, auto &&f) {
+        if (!(wanted >> v & 1)) return;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            f32x4 s = *place(v, p, half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += f(4 * half + e);
+            *place(v, p, half) = s;
+        }
+    };
+    const bool with_u = POST || a.read_u;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const int64_t at = axis_offset_fast(a.row, row);
+        float d[P][VEC], t[P][VEC], hat[P][VEC], w[P][VEC];
+        f32x4 st = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (PRE || POST) st = *reinterpret_cast<const f32x4 *>(a.stats + 4 * row);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if (dr) get<TS, VEC>(dr, at + col[p], d[p]);
+            else
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) d[p][e] = 0.f;
+            if constexpr (PRE) {
+                get<TB, VEC>(dn, at + col[p], t[p]);
+                get<TS, VEC>(r, at + col[p], hat[p]);
+            }
+            if (with_u) get<TB, VEC>(u, at + col[p], w[p]);
+        }
+        if constexpr (PRE) {
+            float m[2] = {0.f, 0.f};
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                float gamma[VEC];
+                vector_at<VEC>(a.p.pre_gamma, vec[p], 1.f, gamma);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) hat[p][e] = (hat[p][e] - st[2]) * st[3];
+                add(3, p, [&](int e) { return t[p][e] * hat[p][e]; });
+                add(4, p, [&](int e) { return t[p][e]; });
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    t[p][e] *= gamma[e];
+                    m[0] += live[p] ? t[p][e] : 0.f;
+                    m[1] = fmaf(live[p] ? t[p][e] : 0.f, live[p] ? hat[p][e] : 0.f, m[1]);
+                }
+            }
+            group_sum<2>(g, m);
+            const float m0 = a.pre_kind == CUBE3D_NORM_LAYER ? m[0] * inv : 0.f, m1 = m[1] * inv;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) d[p][e] += st[3] * (t[p][e] - m0 - hat[p][e] * m1);
+        }
+        float m[2] = {0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            if (dx && live[p]) *reinterpret_cast<Pack8<TS> *>(dx + at + col[p]) = pack_out<TS>(d[p]);
+            float gate[VEC];
+            vector_at<VEC>(a.p.gate, vec[p], 1.f, gate);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) d[p][e] *= a.scale;
+            if constexpr (POST) {
+                float gamma[VEC], beta[VEC];
+                vector_at<VEC>(a.p.post_gamma, vec[p], 1.f, gamma);
+                vector_at<VEC>(a.p.post_beta, vec[p], 0.f, beta);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) w[p][e] = (w[p][e] - st[0]) * st[1];
+                add(2, p, [&](int e) { return d[p][e] * (w[p][e] * gamma[e] + beta[e]); });
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) d[p][e] *= gate[e];
+                add(0, p, [&](int e) { return d[p][e] * w[p][e]; });
+                add(1, p, [&](int e) { return d[p][e]; });
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    d[p][e] *= gamma[e];
+                    m[0] += live[p] ? d[p][e] : 0.f;
+                    m[1] = fmaf(live[p] ? d[p][e] : 0.f, live[p] ? w[p][e] : 0.f, m[1]);
+                }
+            } else {
+                if (with_u) add(2, p, [&](int e) { return d[p][e] * w[p][e]; });
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) d[p][e] *= gate[e];
+            }
+        }
+        if constexpr (POST) {
+            group_sum<2>(g, m);
+            const float m0 = a.post_kind == CUBE3D_NORM_LAYER ? m[0] * inv : 0.f, m1 = m[1] * inv;
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) d[p][e] = st[1] * (d[p][e] - m0 - w[p][e] * m1);
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if (du && live[p]) *reinterpret_cast<Pack8<TB> *>(du + at + col[p]) = pack_out<TB>(d[p]);
+    }
+    float *out = partials + (int64_t)blockIdx.x * VECTORS * a.cols;
+#pragma unroll
+    for (int v = 0; v < VECTORS; ++v)
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            if ((wanted >> v & 1) && live[p]) {
+                f32x4 *dst = reinterpret_cast<f32x4 *>(out + (int64_t)v * a.cols + (p * lanes + (int)threadIdx.x) * VEC);
+                dst[0] = *place(v, p, 0);
+                dst[1] = *place(v, p, 1);
+            }
 }
 
 // How rows are dealt out: wavefronts per row, rows per workgroup, pieces of eight columns per lane, workgroups; waves = 0: the row does not
@@ -684,10 +850,9 @@ struct RowPlan {
 RowPlan row_plan(const NormArgs &a, bool backward)
 {
     RowPlan p{0, 1, 1, 0};
-    if (!eights(a)) return p;
-    const int most = backward ? 16 * SHORT_ROW : 32 * SHORT_ROW;
-    if (a.cols > most) return p;
-    p.pieces = !backward && a.cols > 16 * SHORT_ROW ? 2 : 1;
+    if (widest(a) != VEC) return p;
+    if (a.cols > 32 * SHORT_ROW) return p;
+    p.pieces = a.cols > 16 * SHORT_ROW ? 2 : 1;
     p.waves = (a.cols + SHORT_ROW * p.pieces - 1) / (SHORT_ROW * p.pieces);
     const int64_t cus = num_compute_units();
     if (backward) {
@@ -709,7 +874,7 @@ RowPlan row_plan(const NormArgs &a, bool backward)
 // Rows per workgroup of the column pass: enough workgroups for every CU, few enough partial sums.
 int rows_per_group(const NormArgs &a)
 {
-    const int64_t width = eights(a) ? 64 * VEC : 64, tiles = (a.cols + width - 1) / width;
+    const int64_t width = 64 * widest(a), tiles = (a.cols + width - 1) / width;
     int64_t rows = 256;
     while (rows > 16 && tiles * ((a.rows + rows - 1) / rows) < 2048) rows /= 2;
     while ((a.rows + rows - 1) / rows > 32768) rows *= 2;
@@ -723,10 +888,15 @@ template <typename F> int by_types(const NormArgs &a, F &&f)
     return b ? f((unsigned short)0, float{}) : f((unsigned short)0, (unsigned short)0);
 }
 
-unsigned row_grid(int64_t rows)
+// One wavefront a row where it takes at most eight turns, else a workgroup of four; in either case 32 wavefronts a CU.
+// LANES and the number of workgroups are passed to `f`.
+template <typename F> void by_lanes(const NormArgs &a, int v, F &&f)
 {
-    const int64_t most = (int64_t)num_compute_units() * 8;
-    return (unsigned)(rows < most ? rows : most);
+    const bool one = a.cols <= 8 * 64 * v;
+    const int64_t most = (int64_t)num_compute_units() * (one ? 32 : 8);
+    const dim3 groups((unsigned)(a.rows < most ? a.rows : most));
+    if (one) f(std::integral_constant<int, 64>{}, groups);
+    else f(std::integral_constant<int, ROW_LANES>{}, groups);
 }
 
 }  // namespace
@@ -738,11 +908,16 @@ int norm_fwd(const NormArgs &a, hipStream_t stream)
         typedef decltype(s) TS;
         typedef decltype(b) TB;
         const dim3 block(64 * plan.waves * plan.rows_at_once);
-        if (plan.waves == 0 && eights(a))
-            hipLaunchKernelGGL((norm_fwd_rows_kernel<TS, TB, VEC>), dim3(row_grid(a.rows)), dim3(ROW_LANES), 0, stream, a);
-        else if (plan.waves == 0)
-            hipLaunchKernelGGL((norm_fwd_rows_kernel<TS, TB, 1>), dim3(row_grid(a.rows)), dim3(ROW_LANES), 0, stream, a);
-        else if (plan.pieces == 1)
+        if (plan.waves == 0)
+            return by_width(a, [&](auto v) {
+                constexpr int V = decltype(v)::value;
+                by_lanes(a, V, [&](auto l, dim3 groups) {
+                    constexpr int LANES = decltype(l)::value;
+                    hipLaunchKernelGGL((norm_fwd_rows_kernel<TS, TB, V, LANES>), groups, dim3(LANES), 0, stream, a);
+                });
+                return launch_status();
+            });
+        if (plan.pieces == 1)
             hipLaunchKernelGGL((norm_fwd_kernel<TS, TB, 1>), dim3(plan.groups), block, 0, stream, a, plan.waves, plan.rows_at_once);
         else
             hipLaunchKernelGGL((norm_fwd_kernel<TS, TB, 2>), dim3(plan.groups), block, 0, stream, a, plan.waves, plan.rows_at_once);
@@ -750,12 +925,15 @@ int norm_fwd(const NormArgs &a, hipStream_t stream)
     });
 }
 
+// (long rows: whether they fit depends on the vectors asked for, so there is room for either way)
 size_t norm_bwd_workspace(const NormArgs &a)
 {
     const RowPlan plan = row_plan(a, true);
-    if (plan.waves > 0) return (size_t)plan.groups * VECTORS * a.cols * sizeof(float);
+    const size_t in_registers = (size_t)plan.groups * VECTORS * a.cols * sizeof(float);
+    if (plan.waves > 0 && plan.pieces == 1) return in_registers;
     const int64_t per = rows_per_group(a), groups = (a.rows + per - 1) / per;
-    return ((size_t)a.rows * 4 + (size_t)groups * VECTORS * a.cols) * sizeof(float);
+    const size_t by_columns = ((size_t)a.rows * 4 + (size_t)groups * VECTORS * a.cols) * sizeof(float);
+    return by_columns > in_registers ? by_columns : in_registers;
 }
 
 namespace {
@@ -773,7 +951,26 @@ int finish(const NormArgs &a, const float *partials, unsigned groups, const cube
 int norm_bwd(const NormArgs &a, const cube3d_norm_params &gradients, void *workspace, hipStream_t stream)
 {
     const bool pre = a.pre_kind != CUBE3D_NORM_NONE, post = a.post_kind != CUBE3D_NORM_NONE;
-    if (const RowPlan plan = row_plan(a, true); plan.waves > 0) {
+    const cube3d_norm_params &d = gradients;
+    const int wanted = (d.post_gamma ? 1 : 0) | (d.post_beta ? 2 : 0) | (d.gate ? 4 : 0) | (d.pre_gamma ? 8 : 0) | (d.pre_beta ? 16 : 0);
+    const RowPlan plan = row_plan(a, true);
+    if (plan.waves > 0 && plan.pieces == 2 && __builtin_popcount(wanted) * plan.waves * 2 * SHORT_ROW <= LONG_SUMS) {
+        float *partials = static_cast<float *>(workspace);
+        const int rc = by_types(a, [&](auto s, auto b) {
+            typedef decltype(s) TS;
+            typedef decltype(b) TB;
+            auto launch = [&](auto pre_c, auto post_c) {
+                hipLaunchKernelGGL((norm_bwd_long_kernel<TS, TB, decltype(pre_c)::value, decltype(post_c)::value>), dim3(plan.groups),
+                                   dim3(64 * plan.waves), 0, stream, a, partials, plan.waves, wanted);
+                return launch_status();
+            };
+            const std::true_type yes{};
+            const std::false_type no{};
+            return pre ? (post ? launch(yes, yes) : launch(yes, no)) : (post ? launch(no, yes) : launch(no, no));
+        });
+        return rc != CUBE3D_OK || !a.sums ? rc : finish(a, partials, plan.groups, gradients, stream);
+    }
+    if (plan.waves > 0 && plan.pieces == 1) {
         float *partials = static_cast<float *>(workspace);
         const dim3 grid(plan.groups), block(64 * plan.waves * plan.rows_at_once);
         const size_t lds = plan.rows_at_once > 1 ? sizeof(float) * plan.rows_at_once * plan.waves * SHORT_ROW : 0;
@@ -802,15 +999,18 @@ int norm_bwd(const NormArgs &a, const cube3d_norm_params &gradients, void *works
     const int rc = by_types(a, [&](auto s, auto b) {
         typedef decltype(s) TS;
         typedef decltype(b) TB;
-        auto launch = [&](auto v) {
+        return by_width(a, [&](auto v) {
             constexpr int V = decltype(v)::value;
-            if (pre || post) hipLaunchKernelGGL((norm_bwd_rows_kernel<TS, TB, V>), dim3(row_grid(a.rows)), dim3(ROW_LANES), 0, stream, a, scalars);
+            if (pre || post)
+                by_lanes(a, V, [&](auto l, dim3 wide) {
+                    constexpr int LANES = decltype(l)::value;
+                    hipLaunchKernelGGL((norm_bwd_rows_kernel<TS, TB, V, LANES>), wide, dim3(LANES), 0, stream, a, scalars);
+                });
             if (const int e = launch_status(); e != CUBE3D_OK) return e;
             hipLaunchKernelGGL((norm_bwd_columns_kernel<TS, TB, V>), dim3((unsigned)((a.cols + 64 * V - 1) / (64 * V)), groups), dim3(256), 0,
                                stream, a, scalars, partials, per);
             return launch_status();
-        };
-        return eights(a) ? launch(std::integral_constant<int, VEC>{}) : launch(std::integral_constant<int, 1>{});
+        });
     });
     return rc != CUBE3D_OK || !a.sums ? rc : finish(a, partials, groups, gradients, stream);
 }
