@@ -220,7 +220,7 @@ template <int SIDE, typename Acc, int NBM, int NBN, int ROOM, bool AHEAD, bool S
         // a fixed distance apart; the others ask the map row by row (a 64-bit multiplication takes 16 cycles, a map three of them).
         int64_t all_cols[GROUPS], pass_row[PASSES];
 #pragma unroll
-        for (int j = 0; j < GROUPS; ++j) all_cols[j] = axis_offset_fast(p.maps.c_n, min(n0 + j * COLS + rd_col, p.No - 1));
+        for (int j = 0; j < GROUPS; ++j) all_cols[j] = axis_offset_fast(p.maps.c_n, max(min(n0 + j * COLS + rd_col, p.No - CW), 0));
 #pragma unroll
         for (int ps = 0; ps < PASSES; ++ps) pass_row[ps] = (ps * RPP + rd_row) * row_step;
         struct At {
@@ -247,7 +247,7 @@ template <int SIDE, typename Acc, int NBM, int NBN, int ROOM, bool AHEAD, bool S
         };
         constexpr int HELD = EARLY ? PASSES : 1;
         typename Run::Residual residual[HELD];
-        // (rows and columns beyond the output load what lies at its end)
+        // (lanes beyond the output load the last row's or the last CW columns)
         auto load = [&](const At &x, int ps, typename Run::Residual &res) {
             if (KIND != PLAIN && KIND != WITH_Z && whole) Run::template load<KIND>(p.e, offset(x, ps), res);
         };
