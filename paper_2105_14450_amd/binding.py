@@ -71,6 +71,7 @@ class Epilogue(ctypes.Structure):
     """Mirror of ``cube3d_epilogue``; keeps the tensors it points to alive."""
     _fields_ = [("activation", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("z_dtype", ctypes.c_int32),
                 ("bias_diag", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("z", ctypes.c_void_p)]
+    tensors = ()
 
 
 class Norm(ctypes.Structure):
@@ -82,6 +83,7 @@ class Norm(ctypes.Structure):
 class NormParams(ctypes.Structure):
     """Mirror of ``cube3d_norm_params``; keeps the tensors it points to alive."""
     _fields_ = [(name, ctypes.c_void_p) for name in ("post_gamma", "post_beta", "gate", "pre_gamma", "pre_beta")]
+    tensors = ()
 
 
 class Tensor(ctypes.Structure):
@@ -111,8 +113,13 @@ class TensorList:
 
     def __init__(self, tensors, dtypes):
         self.tensors, self.count = tuple(tensors), len(tensors)
-        self.array = (Tensor * max(1, self.count))(*[Tensor(_ptr(t) if t.numel() else None, t.numel(), code)
-                                                    for t, code in zip(tensors, dtypes)])
+        elements = []
+        for t, code in zip(tensors, dtypes):
+            if code not in ELEM_SIZE or t.numel() * t.element_size() % ELEM_SIZE[code]:
+                raise ValueError("whole elements of a dtype code each")
+            elements.append(t.numel() * t.element_size() // ELEM_SIZE[code])
+        self.array = (Tensor * max(1, self.count))(*[Tensor(_ptr(t) if n else None, n, code)
+                                                    for t, n, code in zip(tensors, elements, dtypes)])
 
 
 def make_tensor_list(tensors, dtypes=None) -> TensorList:
@@ -253,6 +260,34 @@ def _ptr(t):
     if not t.is_contiguous():
         raise ValueError("tensors must be contiguous")
     return t.data_ptr()
+
+
+def _one_device():
+    """Whether the process sees one device only: no tensor can be on another one then (asked once)."""
+    global _only_device
+    if _only_device is None:
+        import torch
+        _only_device = torch.cuda.device_count() <= 1
+    return _only_device
+
+
+_only_device = None
+
+
+def _current_device():
+    import torch
+    return torch.cuda.current_device()
+
+
+def _check_device(tensors, stream):
+    """The kernels run on the calling thread's current device, on a stream of it."""
+    if _one_device():
+        return
+    here = _current_device()
+    if any(t is not None and t.numel() and t.get_device() != here for t in tensors):
+        raise ValueError("tensors must be on the current device")
+    if stream is not None and stream.device_index != here:
+        raise ValueError("the stream must be one of the current device")
 
 
 def _stream(stream):
@@ -425,6 +460,7 @@ def cube3d_epilogue_workspace_bytes(desc: Desc, op: int) -> int:
 
 
 def virtual_cube_linear_fwd_fused(desc, epilogue, X_shards, W_shards, Y_shards, workspace=None, stream=None):
+    _check_device((X_shards, W_shards, Y_shards, workspace) + epilogue.tensors, stream)
     _check(load().virtual_cube_linear_fwd_fused(ctypes.byref(desc), ctypes.byref(epilogue), _ptr(X_shards), _ptr(W_shards),
                                                 _ptr(Y_shards), _ptr(workspace), _bytes(workspace), _stream(stream)),
            "virtual_cube_linear_fwd_fused")
@@ -433,6 +469,7 @@ def virtual_cube_linear_fwd_fused(desc, epilogue, X_shards, W_shards, Y_shards, 
 
 def virtual_cube_linear_epilogue_bwd(desc, kind, z_dtype, dy_dtype, dz_dtype, Z_shards, dY_shards, dZ_shards, dbias_diag=None,
                                      workspace=None, stream=None):
+    _check_device((Z_shards, dY_shards, dZ_shards, dbias_diag, workspace), stream)
     _check(load().virtual_cube_linear_epilogue_bwd(ctypes.byref(desc), kind, z_dtype, dy_dtype, dz_dtype, _ptr(Z_shards),
                                                    _ptr(dY_shards), _ptr(dZ_shards), _ptr(dbias_diag), _ptr(workspace),
                                                    _bytes(workspace), _stream(stream)), "virtual_cube_linear_epilogue_bwd")
@@ -444,12 +481,14 @@ def cube3d_norm_workspace_bytes(m: Matrix, norm: Norm) -> int:
 
 
 def virtual_cube_norm_fwd(m, norm, params, x, u, r, n, stats=None, stream=None):
+    _check_device((x, u, r, n, stats) + params.tensors, stream)
     _check(load().virtual_cube_norm_fwd(ctypes.byref(m), ctypes.byref(norm), ctypes.byref(params), _ptr(x), _ptr(u), _ptr(r),
                                         _ptr(n), _ptr(stats), _stream(stream)), "virtual_cube_norm_fwd")
     return r, n
 
 
 def virtual_cube_norm_bwd(m, norm, params, stats, dr, dn, r, u, dx, du, gradients, workspace, stream=None):
+    _check_device((stats, dr, dn, r, u, dx, du, workspace) + params.tensors + gradients.tensors, stream)
     _check(load().virtual_cube_norm_bwd(ctypes.byref(m), ctypes.byref(norm), ctypes.byref(params), _ptr(stats), _ptr(dr), _ptr(dn),
                                         _ptr(r), _ptr(u), _ptr(dx), _ptr(du), ctypes.byref(gradients), _ptr(workspace),
                                         _bytes(workspace), _stream(stream)), "virtual_cube_norm_bwd")
@@ -460,7 +499,15 @@ def cube3d_grad_norm_workspace_bytes(grads: TensorList) -> int:
     return int(load().cube3d_grad_norm_workspace_bytes(grads.array, grads.count))
 
 
+def _check_scalar(t, size, what):
+    if t is not None and (t.numel() == 0 or t.element_size() != size):
+        raise ValueError(what)
+
+
 def cube3d_grad_norm(grads, sumsq, norm=None, workspace=None, scale=1.0, stream=None):
+    _check_scalar(sumsq, 8, "sumsq is a float64")
+    _check_scalar(norm, 4, "norm is a float32")
+    _check_device(grads.tensors + (sumsq, norm, workspace), stream)
     _check(load().cube3d_grad_norm(grads.array, grads.count, scale, _ptr(sumsq), _ptr(norm), _ptr(workspace), _bytes(workspace),
                                    _stream(stream)), "cube3d_grad_norm")
     return norm
@@ -469,6 +516,8 @@ def cube3d_grad_norm(grads, sumsq, norm=None, workspace=None, scale=1.0, stream=
 def cube3d_grad_clip(grads, out, sumsq, max_norm, scale=1.0, stream=None):
     if out.count != grads.count:
         raise ValueError("as many results as gradients")
+    _check_scalar(sumsq, 8, "sumsq is a float64")
+    _check_device(grads.tensors + out.tensors + (sumsq,), stream)
     _check(load().cube3d_grad_clip(grads.array, out.array, grads.count, scale, max_norm, _ptr(sumsq), _stream(stream)),
            "cube3d_grad_clip")
     return out

@@ -620,7 +620,8 @@ int check_norm(const cube3d_matrix *m, const cube3d_norm *norm, NormArgs *out)
     if (rc != CUBE3D_OK) return rc;
     if (m->row_axis != CUBE3D_AXIS_X || m->split != CUBE3D_SPLIT_ROWS) return CUBE3D_EINVAL;
     if (m->cols % ((int64_t)m->q * m->q)) return CUBE3D_ESHAPE;
-    if (m->rows >= (1ll << 31) || m->cols >= (1ll << 31)) return CUBE3D_ESHAPE;
+    // (the kernels count columns in 32 bits, by up to 8192 past the end)
+    if (m->rows >= (1ll << 31) || m->cols > (1ll << 31) - (1 << 16)) return CUBE3D_ESHAPE;
     if (!norm) return CUBE3D_EINVAL;
     if (!f32_or_bf16(m->dtype) || !f32_or_bf16(norm->block_dtype)) return CUBE3D_EDTYPE;
     for (int kind : {norm->post_kind, norm->pre_kind})
@@ -806,6 +807,10 @@ int virtual_cube_norm_bwd(const cube3d_matrix *m, const cube3d_norm *norm, const
     for (const void *in : {dn, r, u})
         if (in && (in == dx || in == du)) return CUBE3D_EINVAL;
     if (du && (du == dr || du == dx)) return CUBE3D_EINVAL;
+    const float *vectors[] = {d.post_gamma, d.post_beta, d.gate, d.pre_gamma, d.pre_beta};
+    for (int i = 0; i < 5; ++i)
+        for (int k = 0; k < i; ++k)
+            if (vectors[i] && vectors[i] == vectors[k]) return CUBE3D_EINVAL;
     if (!workspace || workspace_bytes < norm_bwd_workspace(a)) return CUBE3D_EWORKSPACE;
     a.p = used_params(*norm, *params, u != nullptr);
     a.x = r; a.u = u;

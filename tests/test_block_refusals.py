@@ -183,3 +183,17 @@ def test_results_of_clipping_may_not_overlap(lib):
                  ([(X, 64, f), (W, 64, f)], [(X, 64, f), (X + 128, 64, f)]),              # inside another one
                  ([(X, 4, f), (W, 64, f)], [(W + 240, 4, f), (Y, 64, f)])):               # on the end of another gradient
         assert clip(g, o) == c3.EINVAL, (g, o)
+
+
+def test_norm_sizes_and_gradients_in_one_place(lib):
+    nd = c3.make_norm(pre=c3.NORM_RMS)
+    for cols, status in (((1 << 31) - 1, c3.ESHAPE), ((1 << 31) - (1 << 16) + 1, c3.ESHAPE), ((1 << 31) - (1 << 16), c3.EINVAL)):
+        m = matrix(q=1, rows=1, cols=cols)      # (the last one is refused for its arguments)
+        assert lib.virtual_cube_norm_fwd(ctypes.byref(m), ctypes.byref(nd), ctypes.byref(NOTHING), None, None, None, N, None, None) == status
+    nd = c3.make_norm(pre=c3.NORM_LAYER, post=c3.NORM_LAYER)
+    names = [f[0] for f in b.NormParams._fields_]
+    for i, first in enumerate(names):
+        for second in names[:i]:
+            g = b.NormParams(**{first: A, second: A})
+            assert lib.virtual_cube_norm_bwd(ctypes.byref(matrix()), ctypes.byref(nd), ctypes.byref(NOTHING), E, X, N, R, U, Y, D,
+                                             ctypes.byref(g), WS, 1 << 40, None) == c3.EINVAL
