@@ -427,7 +427,9 @@ int cube3d_activation_bwd(int kind, int z_dtype, int dh_dtype, int dz_dtype, int
  *   residual     NULL, or R as a cube of Y shards of residual_dtype (F32 or BF16).  May be Y itself if the two
  *                types agree: the sum is then formed in place
  *   z            NULL, or where Z goes: a cube of Y shards of z_dtype (F32 or BF16), for the backward pass
- * (residual_dtype and z_dtype are ignored where their pointer is NULL.)  Products of few tokens are split along the
+ * (residual_dtype and z_dtype are ignored where their pointer is NULL.)  Where Y or Z is fp32, fp8 operands are widened to bf16
+ * on their way into the matrix units, whose fp8 instructions add in fewer bits than fp32 (1.5e-5 of the result's
+ * norm off; to be seen in an fp32 result only, and at twice the time).  Products of few tokens are split along the
  * contraction and joined in `workspace`: device scratch, 16-byte aligned, of at least
  * cube3d_epilogue_workspace_bytes(desc, CUBE3D_OP_FWD) bytes (may be NULL when that is 0, else CUBE3D_EWORKSPACE);
  * contents undefined afterwards.  The order of an element's sum is fixed by the shape: two calls give the same bits.

@@ -113,6 +113,10 @@ int run_gemm(const GemmArgs &a)
             if (need > 0 && (!a.workspace || a.workspace_bytes < need)) return CUBE3D_EWORKSPACE;
             return gemm_rows(a, splits);
         }
+        if (widens(a)) {        // (not by the tuned kernel, which has the fp8 instructions only)
+            const int rc = gemm_edge(a);
+            return rc == CUBE3D_ENOTIMPL ? gemm_generic(a) : rc;
+        }
     }
     const FastPlan plan = gemm_fast_plan(a);
     const size_t need = gemm_fast_workspace(a, plan);

@@ -28,6 +28,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
@@ -123,6 +124,14 @@ struct GemmArgs {
     // nullptr, or what follows the product (forward layout with maps, batch 1)
     const Epilogue *epilogue;
 };
+
+// Whether the product's fp8 operands are widened to bf16 (exact): where what follows it stores an fp32 result.  The fp8 matrix
+// instructions add products of one step in fewer bits than fp32 has: 1.5e-5 of a result's norm off at any length, a hundredth of a
+// bf16 rounding, but a hundred times what fp32 sums are off (1e-7 for 512 products, 6e-7 for 8192).
+inline bool widens(const GemmArgs &g)
+{
+    return g.epilogue && g.in_dtype == CUBE3D_FP8_E4M3 && (g.out_dtype == CUBE3D_F32 || (g.epilogue->z && g.epilogue->z_f32));
+}
 
 // Any shape, any supported dtype; bounds-checked.  Returns a cube3d_status.
 int gemm_generic(const GemmArgs &g);

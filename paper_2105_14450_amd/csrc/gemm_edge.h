@@ -39,7 +39,6 @@
 namespace cube3d {
 namespace edge {
 
-typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int BKB = 128;      // bytes of contraction index per K-tile and row
@@ -159,6 +158,26 @@ struct Fp8 {
     }
 };
 
+// fp8 operands in fp32 sums (widens): as above with the fragments widened on their way into the bf16 instructions, which place
+// indices and outputs alike.  For the kernels with what follows the product only.  us with Z in bf16 / in fp32, where the 16-deep
+// bf16 instructions and the conversions bound it: 8192 x 2048 x 8192 164 / 364, 2997 x 1152 x 4608 38 / 75, 1024 x 2048 x 2048 15 / 18.
+struct Fp8Wide {
+    static constexpr int ELT = 1;
+    __device__ static __forceinline__ int mn_swz(int k, int spr) { return Fp8::mn_swz(k, spr); }
+    struct M32 : Fp8::M32 {
+        __device__ static __forceinline__ Acc mfma(Frag a, Frag b, Acc c, int)
+        {
+            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen_fp8(a), widen_fp8(b), c, 0, 0, 0);
+        }
+    };
+    struct M16 : Fp8::M16 {
+        __device__ static __forceinline__ Acc mfma(Frag a, Frag b, Acc c, int)
+        {
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen_fp8(a), widen_fp8(b), c, 0, 0, 0);
+        }
+    };
+};
+
 struct F32 {
     static constexpr int ELT = 4;
     __device__ static __forceinline__ int mn_swz(int k, int spr) { return spr >= 16 ? 8 * ((k >> 2) & 1) : 0; }
@@ -199,6 +218,10 @@ template <> struct Instr<Bf16, 32> {
 };
 template <> struct Instr<Fp8, 32> {
     typedef Fp8::M16 M;
+    static constexpr int KW = 1;
+};
+template <> struct Instr<Fp8Wide, 32> {
+    typedef Fp8Wide::M16 M;
     static constexpr int KW = 1;
 };
 template <> struct Instr<F32, 32> {
@@ -380,10 +403,13 @@ template <typename E, int T, int GB> int launch_layout(const GemmArgs &g, const 
         hipLaunchKernelGGL((gemm_edge_epilogue_kernel<E, T, GB, true, false>), grid, block, 0, g.stream, epilogue_params(g, p));
         return launch_status();
     }
-    if (g.a_kmajor && g.b_kmajor) hipLaunchKernelGGL((gemm_edge_kernel<E, T, GB, true, true>), grid, block, 0, g.stream, p);
-    else if (g.a_kmajor) hipLaunchKernelGGL((gemm_edge_kernel<E, T, GB, true, false>), grid, block, 0, g.stream, p);
-    else hipLaunchKernelGGL((gemm_edge_kernel<E, T, GB, false, false>), grid, block, 0, g.stream, p);
-    return launch_status();
+    if constexpr (std::is_same<E, Fp8Wide>::value) return CUBE3D_EINVAL;
+    else {
+        if (g.a_kmajor && g.b_kmajor) hipLaunchKernelGGL((gemm_edge_kernel<E, T, GB, true, true>), grid, block, 0, g.stream, p);
+        else if (g.a_kmajor) hipLaunchKernelGGL((gemm_edge_kernel<E, T, GB, true, false>), grid, block, 0, g.stream, p);
+        else hipLaunchKernelGGL((gemm_edge_kernel<E, T, GB, false, false>), grid, block, 0, g.stream, p);
+        return launch_status();
+    }
 }
 
 template <typename E, int GB> int launch_tile(const GemmArgs &g, const Params &p, int tile)
@@ -399,10 +425,12 @@ template <typename E, int GB> int launch_tile(const GemmArgs &g, const Params &p
 // per element type, in a translation unit of its own (piece = bytes per load as chosen by gemm_edge)
 int gemm_edge_bf16(const GemmArgs &g, const edge::Params &p, int tile, int piece);
 int gemm_edge_fp8(const GemmArgs &g, const edge::Params &p, int tile, int piece);
+int gemm_edge_fp8_wide(const GemmArgs &g, const edge::Params &p, int tile, int piece);
 int gemm_edge_f32(const GemmArgs &g, const edge::Params &p, int tile, int piece);
 int gemm_ring_bf16(const GemmArgs &g, const edge::Params &p, const edge::RingPlan &r);
 int gemm_ring_fp8(const GemmArgs &g, const edge::Params &p, const edge::RingPlan &r);
 int gemm_ring_fp8_deep(const GemmArgs &g, const edge::Params &p, const edge::RingPlan &r);
+int gemm_ring_fp8_wide(const GemmArgs &g, const edge::Params &p, const edge::RingPlan &r);
 int gemm_ring_f32(const GemmArgs &g, const edge::Params &p, const edge::RingPlan &r);
 
 }  // namespace cube3d

@@ -259,7 +259,8 @@ RingPlan ring_plan(const GemmArgs &g, const Plan &plan)
     // Few rows in fp32: the wavefronts of a 32 x 32 tile share its k-steps, a quarter of the chain (10 x 384 x 3904: 28 us, 69 on
     // the ring's tiles of 64).  One K-tile of 256 bytes: nothing to keep in flight (85 x 448 x 128 fp8 4.5 against 4.7 us).
     if (plan.tile == 32 && (f32 || g.Kc * es <= 256)) return best;
-    const bool wide = g.out_dtype == CUBE3D_F32, kk = g.a_kmajor && g.b_kmajor;
+    // (fp8 operands widened: the 16-deep MFMAs of fp32 results)
+    const bool wide = g.out_dtype == CUBE3D_F32 || widens(g), kk = g.a_kmajor && g.b_kmajor;
     const RingCost *costs = f32 ? RING_F32 : fp8 ? (wide ? RING_FP8_F32 : RING_FP8) : RING_BF16;
     const int n = f32 ? 2 : 5;
     const int64_t cus = num_compute_units();
@@ -327,6 +328,7 @@ int gemm_edge(const GemmArgs &g)
         case CUBE3D_F32: return gemm_ring_f32(g, plan.params, ring);
         case CUBE3D_BF16: return gemm_ring_bf16(g, plan.params, ring);
         default:
+            if (widens(g)) return gemm_ring_fp8_wide(g, plan.params, ring);
             // The 64-deep MFMAs add in another order than the 16-deep ones of all other kernels for any size: where the
             // result is rounded to bf16 and the matrix cores are what bounds the tile.
             return ring.tile_m >= 128 && g.out_dtype == CUBE3D_BF16 ? gemm_ring_fp8_deep(g, plan.params, ring)
@@ -336,7 +338,8 @@ int gemm_edge(const GemmArgs &g)
     switch (g.in_dtype) {
     case CUBE3D_F32: return gemm_edge_f32(g, plan.params, plan.tile, plan.piece);
     case CUBE3D_BF16: return gemm_edge_bf16(g, plan.params, plan.tile, plan.piece);
-    default: return gemm_edge_fp8(g, plan.params, plan.tile, plan.piece);
+    default:
+        return widens(g) ? gemm_edge_fp8_wide(g, plan.params, plan.tile, plan.piece) : gemm_edge_fp8(g, plan.params, plan.tile, plan.piece);
     }
 }
 

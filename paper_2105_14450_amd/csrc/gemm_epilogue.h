@@ -6,6 +6,18 @@
 
 namespace cube3d {
 
+// Eight fp8 codes as bf16, exactly
+__device__ __forceinline__ bf16x8 widen_fp8(i32x2 codes)
+{
+    i32x4 wide;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        wide[2 * i] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)codes[i], 1.f, false));
+        wide[2 * i + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)codes[i], 1.f, true));
+    }
+    return __builtin_bit_cast(bf16x8, wide);
+}
+
 // GELU where nothing hides its arithmetic: z Phi(z) = max(z, 0) - t Phi(-t) with t = |z|, and Phi(-t) = 2^(-p(t)), p(t) = 1 + t
 // times a degree-6 polynomial (equal-ripple fit of -log2 Phi(-t) on [0, 6]; beyond, p keeps growing: 30 at 6).  15 issue slots an
 // element (v_exp_f32 counts four) for the 25 of act_value, which is closer: t Phi(-t) is within 7e-7 here and Phi(-t) within

@@ -6,7 +6,9 @@
 // (4 wavefronts) makes a 64x64 output tile; each wavefront owns one 32x32 MFMA accumulator.
 //
 // Implements the local products of Algorithm 1 step 3 and Algorithm 2 lines 1-2.
-#include "activation.h"
+#include <type_traits>
+
+#include "gemm_epilogue.h"
 
 namespace cube3d {
 namespace {
@@ -52,6 +54,13 @@ __device__ __forceinline__ f32x16 mfma_step<unsigned char>(const unsigned char *
     return __builtin_amdgcn_mfma_f32_32x32x16_fp8_fp8(a, b, acc, 0, 0, 0);
 }
 
+__device__ __forceinline__ f32x16 mfma_step_wide(const unsigned char *arow, const unsigned char *brow, int kk, int khalf, f32x16 acc)
+{
+    const i32x2 a = *reinterpret_cast<const i32x2 *>(arow + kk + 8 * khalf);
+    const i32x2 b = *reinterpret_cast<const i32x2 *>(brow + kk + 8 * khalf);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen_fp8(a), widen_fp8(b), acc, 0, 0, 0);
+}
+
 template <typename TOut> __device__ __forceinline__ void store_out(TOut *p, float v);
 template <> __device__ __forceinline__ void store_out<float>(float *p, float v) { *p = v; }
 template <> __device__ __forceinline__ void store_out<unsigned short>(unsigned short *p, float v)
@@ -61,8 +70,8 @@ template <> __device__ __forceinline__ void store_out<unsigned short>(unsigned s
 
 // MAPPED: every element address goes through the index maps (operands and output are cubes of
 // shards, Section 3.1.1) and the optional bias is added; the leading dimensions are unused.  EPI: and what follows the
-// product is applied.
-template <typename TIn, typename TOut, bool AK, bool BK, bool MAPPED, bool EPI = false>
+// product is applied.  WIDE: fp8 operands widened to bf16.
+template <typename TIn, typename TOut, bool AK, bool BK, bool MAPPED, bool EPI = false, bool WIDE = false>
 __global__ __launch_bounds__(256) void gemm_generic_kernel(const TIn *__restrict__ A, const TIn *__restrict__ B,
                                                            TOut *__restrict__ C, int64_t Mo, int64_t No, int64_t Kc,
                                                            int64_t lda, int64_t ldb, int64_t ldc, int64_t sA,
@@ -128,7 +137,10 @@ __global__ __launch_bounds__(256) void gemm_generic_kernel(const TIn *__restrict
         }
         __syncthreads();
 #pragma unroll
-        for (int kk = 0; kk < TK; kk += Elem<TIn>::KSTEP) acc = mfma_step<TIn>(arow, brow, kk, khalf, acc);
+        for (int kk = 0; kk < TK; kk += Elem<TIn>::KSTEP) {
+            if constexpr (WIDE) acc = mfma_step_wide(arow, brow, kk, khalf, acc);
+            else acc = mfma_step<TIn>(arow, brow, kk, khalf, acc);
+        }
         __syncthreads();
     }
 
@@ -164,9 +176,16 @@ int launch_layout(const GemmArgs &g)
     const Epilogue epi = g.epilogue ? *g.epilogue : Epilogue{};
     if (g.epilogue) {
         if (!g.maps || g.batch != 1 || !g.a_kmajor || g.b_kmajor) return CUBE3D_EINVAL;
-        hipLaunchKernelGGL((gemm_generic_kernel<TIn, TOut, true, false, true, true>), grid, block, 0, g.stream, A, B, C, g.Mo, g.No, g.Kc,
-                           g.lda, g.ldb, g.ldc, g.strideA, g.strideB, g.strideC, g.alpha, maps, epi);
-        return launch_status();
+        auto launch = [&](auto wide) {
+            hipLaunchKernelGGL((gemm_generic_kernel<TIn, TOut, true, false, true, true, decltype(wide)::value>), grid, block, 0, g.stream, A, B, C,
+                               g.Mo, g.No, g.Kc, g.lda, g.ldb, g.ldc, g.strideA, g.strideB, g.strideC, g.alpha, maps, epi);
+            return launch_status();
+        };
+        if constexpr (sizeof(TIn) == 1) {
+            if (widens(g)) return launch(std::true_type{});
+            if (sizeof(TOut) == 4) return CUBE3D_EINVAL;        // (widened always)
+        }
+        return launch(std::false_type{});
     }
 #define CUBE3D_LAUNCH(AKV, BKV, MP)                                                                               \
     hipLaunchKernelGGL((gemm_generic_kernel<TIn, TOut, AKV, BKV, MP>), grid, block, 0, g.stream, A, B, C, g.Mo, \

@@ -42,7 +42,6 @@ namespace cube3d {
 namespace mfk {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int WAVES = 4;
 

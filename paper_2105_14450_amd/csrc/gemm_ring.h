@@ -208,6 +208,7 @@ __device__ __forceinline__ Place place_item(const Params &p, int id, int TM, int
 template <typename E, int T> struct RingInstr { typedef typename E::M32 M; };
 template <> struct RingInstr<Bf16, 32> { typedef Bf16::M16 M; };
 template <> struct RingInstr<Fp8, 32> { typedef Fp8::M16 M; };
+template <> struct RingInstr<Fp8Wide, 32> { typedef Fp8Wide::M16 M; };
 
 // Output of a wavefront's blocks, JH of them side by side at a time through a strip of LDS of its own: a lane's accumulator
 // holds row lane % SIDE and columns 8 (v / 4) + 4 (lane / SIDE) + v % 4 of a block (operands exchanged in the MFMA) and
@@ -346,10 +347,13 @@ template <typename E, int TM, int TN, int NST> int ring_layout(const GemmArgs &g
             hipLaunchKernelGGL((gemm_ring_epilogue_kernel<E, TM, TN, NST, true, false, S>), grid, block, 0, g.stream, epilogue_params(g, p));
             return launch_status();
         }
-        if (g.a_kmajor && g.b_kmajor) hipLaunchKernelGGL((gemm_ring_kernel<E, TM, TN, NST, true, true, S>), grid, block, 0, g.stream, p);
-        else if (g.a_kmajor) hipLaunchKernelGGL((gemm_ring_kernel<E, TM, TN, NST, true, false, S>), grid, block, 0, g.stream, p);
-        else hipLaunchKernelGGL((gemm_ring_kernel<E, TM, TN, NST, false, false, S>), grid, block, 0, g.stream, p);
-        return launch_status();
+        if constexpr (std::is_same<E, Fp8Wide>::value) return (int)CUBE3D_EINVAL;
+        else {
+            if (g.a_kmajor && g.b_kmajor) hipLaunchKernelGGL((gemm_ring_kernel<E, TM, TN, NST, true, true, S>), grid, block, 0, g.stream, p);
+            else if (g.a_kmajor) hipLaunchKernelGGL((gemm_ring_kernel<E, TM, TN, NST, true, false, S>), grid, block, 0, g.stream, p);
+            else hipLaunchKernelGGL((gemm_ring_kernel<E, TM, TN, NST, false, false, S>), grid, block, 0, g.stream, p);
+            return launch_status();
+        }
     };
     if constexpr (TM * TN > 128 * 128) {
         if (ring_streams(g, p, RingPlan{TM, TN, 0.f})) return launch(std::true_type{});

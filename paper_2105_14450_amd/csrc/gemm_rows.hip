@@ -22,8 +22,6 @@ namespace cube3d {
 
 namespace {
 
-typedef int i32x2 __attribute__((ext_vector_type(2)));
-
 constexpr int COLS = 128, KSTEP = 32, WAVES = 4, MOST_ROWS = 64;
 
 struct RowsParams {
@@ -81,6 +79,14 @@ struct Fp8Rows {
     __device__ static __forceinline__ f32x4 mfma(Frag a, Frag b, f32x4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(__builtin_bit_cast(long, a), __builtin_bit_cast(long, b), c, 0, 0, 0);
+    }
+};
+
+// fp32 results: the operands widened to bf16, whose instruction has the same layout (see widens)
+struct Fp8WideRows : Fp8Rows {
+    __device__ static __forceinline__ f32x4 mfma(Frag a, Frag b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen_fp8(a), widen_fp8(b), c, 0, 0, 0);
     }
 };
 
@@ -300,7 +306,8 @@ int gemm_rows(const GemmArgs &g, int splits)
     p.row_bytes = p.maps.b_k.u * (g.in_dtype == CUBE3D_BF16 ? 2 : 1);
     p.e = *g.epilogue;
     epilogue_pieces(g, &p.piece, &p.bias_piece);
-    return g.in_dtype == CUBE3D_BF16 ? launch_rows<Bf16Rows>(p, g.stream) : launch_rows<Fp8Rows>(p, g.stream);
+    if (g.in_dtype == CUBE3D_BF16) return launch_rows<Bf16Rows>(p, g.stream);
+    return widens(g) ? launch_rows<Fp8WideRows>(p, g.stream) : launch_rows<Fp8Rows>(p, g.stream);
 }
 
 }  // namespace cube3d

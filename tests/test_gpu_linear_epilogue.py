@@ -301,3 +301,30 @@ def test_epilogue_bwd_types(zt, gt, dt, N):
         epilogue_bwd(2, "z", 64, N, act, zt, gt, dt, dist, with_db=False)
         if gt == dt:
             epilogue_bwd(1, "z", 64, N, act, zt, gt, dt, dist, in_place=True)
+
+
+# the ring's tiles of 32, 64, 128 and more; loads of 4 and of single bytes; few rows with and without runs; short contractions
+@pytest.mark.parametrize("q,axis,M,K,N", [(1, "y", 20, 1024, 96), (1, "y", 256, 1024, 512), (1, "z", 1536, 2048, 1024), (1, "y", 2304, 512, 4096),
+                                          (1, "y", 300, 516, 260), (1, "z", 130, 333, 77), (1, "y", 1, 8192, 1024), (1, "y", 40, 6144, 512),
+                                          (1, "y", 7, 24, 40), (1, "y", 4096, 16, 1031), (2, "z", 64, 8192, 512), (3, "y", 999, 1152, 576)])
+@pytest.mark.parametrize("shard,z", [("f32", None), ("bf16", "f32"), ("f32", "f32")])
+def test_fp8_operands_with_fp32_results(q, axis, M, K, N, shard, z):
+    """One product of 2^12 and others that are multiples of 2^-6 below 1: every partial sum is a multiple of 2^-6 below 2^14, so 20
+    bits hold it, and an instruction that adds in fewer drops the small ones next to the large one."""
+    rng = np.random.default_rng(K)
+    X, W = (rng.integers(-7, 8, s) / 8.0 for s in ((M, K), (K, N)))
+    X[:, K // 2] = 64.0
+    W[K // 2] = np.where(np.arange(N) % 2, 64.0, -64.0)
+    assert K * 49 / 64 + 4096 < 2 ** 14
+    codes = lambda v: torch.from_numpy(v).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    layer = Layer(q, axis, M, K, N, "fp8_e4m3", shard=shard)
+    flat = lambda s: gu.to_device(s.reshape((q ** 3,) + s.shape[3:]))
+    layer.x, layer.w = flat(layer.cube.shard_x(codes(X))), flat(layer.cube.shard_w(codes(W)))
+    layer.desc = c3.make_desc(q, M, K, N, in_dtype=c3.FP8_E4M3, shard_dtype=gu.CODE[shard], in_axis=c3.AXIS_Y if axis == "y" else c3.AXIS_Z)
+    layer.z0 = X @ W
+    for residual in (None, "f32"):
+        y, zt, res = layer.run("relu", False, residual, z)
+        if z:
+            np.testing.assert_array_equal(zt, layer.z0)
+        ref = np.maximum(layer.z0, 0.0) + (0.0 if res is None else res)
+        np.testing.assert_array_equal(y, rounded(ref, shard))
