@@ -519,9 +519,8 @@ template <typename TS, typename TB, int P> __global__ __launch_bounds__(1024) vo
     }
 }
 
-// Workgroup w leaves the sums over its rows in partials[w].  MOST: wavefronts of a workgroup.  Both norms at once take some 160
-// registers a lane: eight wavefronts then (2997 x 1152 20.7 us for 45 with sixteen, which spill); where a row needs sixteen the
-// parameters are read row by row and no row ahead (16384 x 8192 482 us for 726).
+// Workgroup w leaves the sums over its rows in partials[w].  MOST: wavefronts of a workgroup (most_waves); with sixteen there are no
+// registers for both norms' parameters, which are read row by row then, and no row ahead.
 template <typename TS, typename TB, bool PRE, bool POST, int MOST>
 __global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, float *__restrict__ partials, int waves, int rows_at_once)
 {
@@ -847,6 +846,16 @@ struct RowPlan {
     unsigned groups;
 };
 
+// Most wavefronts of a backward workgroup.  Both norms at once take some 150 registers a lane: twelve then (in sixteen they spill, or
+// do without what is read ahead), or eight where those hold whole rows and an fp32 stream takes more registers.  us with eight /
+// twelve, at 8192 rows with bf16 and with fp32 streams: 1024 columns 29.0 / 30.3, 31.7 / 34.4; 2048 45.5 / 44.0, 59.6 / 63.3;
+// 2560 81 / 59, 77 / 81; 6144 149 / 129 and 192 / 182 (sixteen / twelve).
+int most_waves(const NormArgs &a, int waves)
+{
+    if (a.pre_kind == CUBE3D_NORM_NONE || a.post_kind == CUBE3D_NORM_NONE || waves > 12) return 16;
+    return waves <= 2 || (waves <= 8 && a.stream_f32) ? 8 : 12;
+}
+
 RowPlan row_plan(const NormArgs &a, bool backward)
 {
     RowPlan p{0, 1, 1, 0};
@@ -858,8 +867,7 @@ RowPlan row_plan(const NormArgs &a, bool backward)
     if (backward) {
         // A workgroup leaves a partial sum of every vector: as few of them as fill the CUs, of as many rows at once as that allows
         // (2997 rows of 1152 with one norm, 62 MB: 45 us with 5 rows at once, 65 with one on five times as many workgroups)
-        const bool both = a.pre_kind != CUBE3D_NORM_NONE && a.post_kind != CUBE3D_NORM_NONE;
-        const int fit = (both && p.waves <= 8 ? 8 : 16) / p.waves;
+        const int fit = most_waves(a, p.waves) / p.waves;
         const int64_t each = (a.rows + cus - 1) / cus;
         p.rows_at_once = fit < each ? fit : (int)each;
     } else p.rows_at_once = p.waves == 1 ? 4 : p.waves == 2 ? 2 : 1;
@@ -979,12 +987,16 @@ int norm_bwd(const NormArgs &a, const cube3d_norm_params &gradients, void *works
             typedef decltype(b) TB;
             auto launch = [&](auto pre_c, auto post_c) {
                 constexpr bool PRE = decltype(pre_c)::value, POST = decltype(post_c)::value;
-                if (PRE && POST && plan.waves <= 8)
-                    hipLaunchKernelGGL((norm_bwd_kernel<TS, TB, PRE, POST, PRE && POST ? 8 : 16>), grid, block, lds, stream, a, partials,
+                auto start = [&](auto most) {
+                    hipLaunchKernelGGL((norm_bwd_kernel<TS, TB, PRE, POST, decltype(most)::value>), grid, block, lds, stream, a, partials,
                                        plan.waves, plan.rows_at_once);
-                else
-                    hipLaunchKernelGGL((norm_bwd_kernel<TS, TB, PRE, POST, 16>), grid, block, lds, stream, a, partials, plan.waves,
-                                       plan.rows_at_once);
+                };
+                if constexpr (PRE && POST) {
+                    const int most = most_waves(a, plan.waves);
+                    if (most == 8) start(std::integral_constant<int, 8>{});
+                    else if (most == 12) start(std::integral_constant<int, 12>{});
+                    else start(std::integral_constant<int, 16>{});
+                } else start(std::integral_constant<int, 16>{});
                 return launch_status();
             };
             const std::true_type yes{};
