@@ -136,8 +136,10 @@ template <int N, bool STREAM = false> struct EpilogueRun {
 // its own in fp32: HR rows of JH blocks at a time, of which a lane reads CW consecutive columns of a row.  A lane's accumulator
 // holds row lane % SIDE and columns 8 (v / 4) + 4 (lane / SIDE) + v % 4 of a block.  The 16-byte slots of a strip row are permuted
 // by the row, so that neither side has bank conflicts.
-// ROOM: bytes of LDS per wavefront.  A strip's values and residuals are read ahead of the next strip's writes (not AHEAD: kernels
-// without registers to spare, only where there is no residual; else they are read pass by pass).
+// ROOM: bytes of LDS per wavefront.  A strip's values and residuals are read ahead of the next strip's writes.  Not AHEAD: kernels
+// without registers to spare, where this holds for one block column and for two without a residual; two with one read a strip's
+// residuals together, and what is left reads pass by pass.  us for read ahead or together / pass by pass: 2997 x 1152 x 4608 with a
+// bf16 residual 50 / 54, 4635 x 576 x 4032 55 / 60, 6000 x 512 x 1000 20.6 / 22.
 template <int SIDE, typename Acc, int NBM, int NBN, int ROOM, bool AHEAD, bool STREAM> struct TileEpilogue {
     static constexpr int VALS = SIDE * SIDE / 64;
     // strips 64 columns wide (whole cache lines of bf16 results), 32 where a wavefront has one block a row, 16 of small tiles
@@ -200,7 +202,7 @@ template <int SIDE, typename Acc, int NBM, int NBN, int ROOM, bool AHEAD, bool S
     {
         asm volatile("" : "+v"(lane));      // (opaque: formed ahead of the K loop, the addresses below would occupy registers all through it)
         typedef EpilogueRun<CW, STREAM> Run;
-        constexpr bool EARLY = AHEAD || KIND == PLAIN || KIND == WITH_Z;
+        constexpr bool EARLY = AHEAD || KIND == PLAIN || KIND == WITH_Z || (KIND != ANY && NBN / JH == 1);
         constexpr int LPR = COLS / CW, RPP = 64 / LPR;              // lanes per strip row, rows per pass
         const int g = lane / SIDE, in_side = lane % SIDE, rd_row = lane / LPR, rd_col = (lane % LPR) * CW;
         constexpr int PASSES = HR / RPP, GROUP = NBM * HALVES, GROUPS = STRIPS / GROUP;     // strips of a block column
@@ -257,7 +259,7 @@ template <int SIDE, typename Acc, int NBM, int NBN, int ROOM, bool AHEAD, bool S
             return x.col_off + (x.simple ? x.first_off + pass_row[ps]
                                          : axis_offset_fast(p.maps.c_m, min(x.first + ps * RPP + rd_row, p.Mo - 1)));
         };
-        constexpr int HELD = EARLY ? PASSES : 1;
+        constexpr int HELD = EARLY || KIND != ANY ? PASSES : 1;
         typename Run::Residual residual[HELD];
         // (lanes beyond the output load the last row's or the last CW columns)
         auto load = [&](const At &x, int ps, typename Run::Residual &res) {
@@ -275,7 +277,7 @@ template <int SIDE, typename Acc, int NBM, int NBN, int ROOM, bool AHEAD, bool S
 #pragma unroll
                 for (int k = 0; k < CW / 4; ++k) {
                     const int r = ps * RPP + rd_row;
-                    t[EARLY ? ps : 0][k] = *reinterpret_cast<const f32x4 *>(strip + r * ROWB + (((rd_col / 4 + k) ^ perm(r)) * 16));
+                    t[HELD > 1 ? ps : 0][k] = *reinterpret_cast<const f32x4 *>(strip + r * ROWB + (((rd_col / 4 + k) ^ perm(r)) * 16));
                 }
             };
             float bias[CW];
@@ -290,9 +292,9 @@ template <int SIDE, typename Acc, int NBM, int NBN, int ROOM, bool AHEAD, bool S
                 const int r = ps * RPP + rd_row;
                 float x[CW];
 #pragma unroll
-                for (int e = 0; e < CW; ++e) x[e] = t[EARLY ? ps : 0][e / 4][e % 4] * p.alpha + bias[e];
+                for (int e = 0; e < CW; ++e) x[e] = t[HELD > 1 ? ps : 0][e / 4][e % 4] * p.alpha + bias[e];
                 if (here.first + r >= p.Mo || here.col >= p.No) return;
-                if (whole) Run::template apply<KIND>(p.e, x, residual[EARLY ? ps : 0], p.C, p.out_f32, offset(here, ps));
+                if (whole) Run::template apply<KIND>(p.e, x, residual[HELD > 1 ? ps : 0], p.C, p.out_f32, offset(here, ps));
                 else Run::apply_some(p.e, x, p.C, p.out_f32, offset(here, ps) - here.col_off, p.maps.c_n, here.col, p.No);
             };
             if constexpr (EARLY) {
@@ -309,11 +311,21 @@ template <int SIDE, typename Acc, int NBM, int NBN, int ROOM, bool AHEAD, bool S
                 for (int ps = 0; ps < PASSES; ++ps) residual[ps] = next[ps];
                 here = there;
             } else {
+                if constexpr (KIND != ANY) {
+#pragma unroll
+                    for (int ps = 0; ps < PASSES; ++ps) load(here, ps, residual[ps]);
+#pragma unroll
+                    for (int ps = 0; ps < PASSES; ++ps) {
+                        read(ps);
+                        finish(ps);
+                    }
+                } else {
 #pragma unroll 1
-                for (int ps = 0; ps < PASSES; ++ps) {
-                    read(ps);
-                    load(here, ps, residual[0]);
-                    finish(ps);
+                    for (int ps = 0; ps < PASSES; ++ps) {
+                        read(ps);
+                        load(here, ps, residual[0]);
+                        finish(ps);
+                    }
                 }
                 if (s + 1 < STRIPS) {
                     write_one_of<0, STRIPS>(s + 1, acc, strip, g, in_side);
