@@ -1,14 +1,15 @@
-// The forward product of few rows (tokens) with what follows it: Y = act(X W + b) + R for M <= 64 over a cube of shards, bf16 and fp8.
+// The forward product of few rows (tokens) with what follows it: Y = act(X W + b) + R for M <= 64 (fp32 32) over a cube of shards.
 //
 // What bounds it: the weights, read once from HBM, M multiply-adds an element.  Nothing is shared between workgroups but X, so W goes
 // from memory straight to registers and into the matrix cores, without LDS, barriers or waits for other wavefronts, and
 // the contraction is cut into as many runs as it takes to have loads in flight on every CU.
 //
-// Tile.  A wavefront makes MT x 16 rows by 128 columns with 16 x 16 x 32 MFMAs.  A k-step is 32 contraction indices: lane l loads
-// W[k0 + 8 (l / 16) + r, n0 + 8 (l % 16) : + 8] for r = 0 ... 7, whole 256-byte (fp8: 128-byte) pieces of a row per 16 lanes, all eight
-// from one lane offset and eight scalar bases.  That is an 8 x 8 block per lane, which byte permutations turn around: column j
-// of the block is the lane's part of the B operand of MFMA number j, whose 16 columns are then n0 + 8 c + j.  X, K-major, is
-// its A operand as stored.  The accumulators of the eight MFMAs hold eight consecutive columns of four rows in a lane.
+// Tile.  A wavefront makes MT x 16 rows by 128 columns with 16 x 16 x 32 MFMAs (fp32: eight of 16 x 16 x 4).  A k-step is 32 contraction
+// indices: lane l loads W[k0 + 8 (l / 16) + r, n0 + 8 (l % 16) : + 8] for r = 0 ... 7, whole 256-byte (fp8: 128, fp32: 512) pieces of
+// a row per 16 lanes, all eight from one lane offset and eight scalar bases.  That is an 8 x 8 block per lane, which byte
+// permutations turn around (fp32: it is only named the other way): column j of the block is the lane's part of the B operand of
+// MFMA number j, whose 16 columns are then n0 + 8 c + j.  X, K-major, is its A operand as stored.  The accumulators of the eight
+// MFMAs hold eight consecutive columns of four rows in a lane.
 //
 // Split.  The four wavefronts of a workgroup take its k-steps in turn, and add up through LDS; the runs of the contraction add up in
 // a second launch, in ascending order (in place of that, one workgroup per strip leaves most CUs without work: 16 to 64 strips of 128
@@ -90,6 +91,25 @@ struct Fp8WideRows : Fp8Rows {
     }
 };
 
+// fp32: the instruction takes four indices, one a group of lanes, so a k-step is eight of them, over the lane's own indices
+struct F32Rows {
+    static constexpr int ELT = 4;
+    typedef float Piece __attribute__((ext_vector_type(8), aligned(16)));
+    typedef Piece Frag;
+    static constexpr int TURN = 1;
+    __device__ static __forceinline__ void turn(const Piece (&row)[8], int c, Frag (&col)[1])
+    {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) col[0][r] = row[r][c];
+    }
+    __device__ static __forceinline__ f32x4 mfma(Frag a, Frag b, f32x4 c)
+    {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], c, 0, 0, 0);
+        return c;
+    }
+};
+
 // Eight columns of row m from column n on: the end of the way, from the full sum.
 __device__ __forceinline__ void finish(const RowsParams &p, int m, int n, float (&x)[8])
 {
@@ -115,7 +135,7 @@ __device__ __forceinline__ void finish(const RowsParams &p, int m, int n, float 
 }
 
 // Grid: strips of 128 columns, runs of the contraction.
-template <typename E, int MT> __global__ __launch_bounds__(64 * WAVES, MT == 4 ? 1 : 2) void gemm_rows_kernel(const RowsParams p)
+template <typename E, int MT> __global__ __launch_bounds__(64 * WAVES, MT == (E::ELT == 4 ? 2 : 4) ? 1 : 2) void gemm_rows_kernel(const RowsParams p)
 {
     typedef typename E::Piece Piece;
     typedef typename E::Frag Frag;
@@ -245,7 +265,9 @@ template <typename E, int MT> int launch(const RowsParams &p, hipStream_t stream
 
 template <typename E> int launch_rows(const RowsParams &p, hipStream_t stream)
 {
-    return p.M <= 16 ? launch<E, 1>(p, stream) : p.M <= 32 ? launch<E, 2>(p, stream) : launch<E, 4>(p, stream);
+    if (p.M <= 16) return launch<E, 1>(p, stream);
+    if constexpr (E::ELT == 4) return launch<E, 2>(p, stream);
+    else return p.M <= 32 ? launch<E, 2>(p, stream) : launch<E, 4>(p, stream);
 }
 
 }  // namespace
@@ -254,10 +276,9 @@ template <typename E> int launch_rows(const RowsParams &p, hipStream_t stream)
 int gemm_rows_plan(const GemmArgs &g)
 {
     if (!g.epilogue || !g.maps || g.batch != 1 || !g.a_kmajor || g.b_kmajor) return 0;
-    if (g.in_dtype != CUBE3D_BF16 && g.in_dtype != CUBE3D_FP8_E4M3) return 0;
-    if (g.Mo > MOST_ROWS || g.No >= 1ll << 24 || g.Kc >= 1ll << 30) return 0;
+    if (g.Mo > (g.in_dtype == CUBE3D_F32 ? MOST_ROWS / 2 : MOST_ROWS) || g.No >= 1ll << 24 || g.Kc >= 1ll << 30) return 0;
     const GemmMaps &m = *g.maps;
-    const int64_t es = g.in_dtype == CUBE3D_BF16 ? 2 : 1;
+    const int64_t es = g.in_dtype == CUBE3D_F32 ? 4 : g.in_dtype == CUBE3D_BF16 ? 2 : 1;
     if (!eights(m.a_k, g.Kc, 1) || !eights(m.b_mn, g.No, 1) || !eights(m.b_k, g.Kc, m.b_k.u) || m.b_k.u % 8) return 0;
     if (m.a_mn.u % 8 || m.a_mn.s1 % 8 || m.a_mn.s2 % 8) return 0;
     // offsets are 32 bits; those of a lane's eight rows lie behind its own
@@ -268,7 +289,12 @@ int gemm_rows_plan(const GemmArgs &g)
     // 14.8 / 32.6, 17.4 / 37.5; 8192 x 8192 32.5 / 37.3, 35.6 / 42.8; fp8 4096 x 4096 10.6 / 11.5, 13.9 / 13.4; 8192 x 2048 11.1 / 18.7,
     // 14.8 / 24.1; 16384 x 4096 (q = 2, 16 rows) 23.3 / 62.9.  64 rows: 4096 x 4096 20.5 / 21.6, 8192 x 2048 21.3 / 36.1, but
     // 12288 x 12288 102 / 90 (fp8 83 / 64): the sums of the runs count.
-    if (g.Kc * es < 6144 || (g.Mo > 32 && g.No > 8192)) return 0;
+    // fp32, where the other kernels' one chain of K-tiles is longer: 512 x 512 7.8 / 9.1 (1 row), 8.6 / 9.3 (16); 2048 x 2048 11.8 / 19.3,
+    // 13.0 / 19.6, 17.2 / 19.8 (32); 8192 x 2048 23 / 58, 24 / 58, 31 / 58; 8192 x 8192 56 / 66, 58 / 67; 32 rows, whose accumulators and
+    // operands leave one wavefront a SIMD, 1024 x 4096 16.2 / 13.7, 2048 x 8192 28 / 23, 8192 x 8192 76 / 66
+    if (g.in_dtype == CUBE3D_F32) {
+        if (g.Kc < (g.Mo > 16 ? 2048 : 512) || (g.Mo > 16 && g.No > 4096)) return 0;
+    } else if (g.Kc * es < 6144 || (g.Mo > 32 && g.No > 8192)) return 0;
     // As many runs as leave the busiest CU the fewest k-steps (20 KB per us and CU), against the traffic of their sums and a launch
     const int64_t strips = (g.No + COLS - 1) / COLS, steps = (g.Kc + KSTEP - 1) / KSTEP, cus = num_compute_units();
     const double step_us = KSTEP * COLS * es / 20.3e3, run_us = (double)g.Mo * g.No * 8 / 5e6;
@@ -303,9 +329,10 @@ int gemm_rows(const GemmArgs &g, int splits)
     p.out_f32 = g.out_dtype == CUBE3D_F32;
     p.maps = *g.maps;
     for (AxisMap *x : {&p.maps.a_mn, &p.maps.a_k, &p.maps.b_mn, &p.maps.b_k, &p.maps.c_m, &p.maps.c_n, &p.maps.bias_n}) prepare_axis_map(*x);
-    p.row_bytes = p.maps.b_k.u * (g.in_dtype == CUBE3D_BF16 ? 2 : 1);
+    p.row_bytes = p.maps.b_k.u * (g.in_dtype == CUBE3D_F32 ? 4 : g.in_dtype == CUBE3D_BF16 ? 2 : 1);
     p.e = *g.epilogue;
     epilogue_pieces(g, &p.piece, &p.bias_piece);
+    if (g.in_dtype == CUBE3D_F32) return launch_rows<F32Rows>(p, g.stream);
     if (g.in_dtype == CUBE3D_BF16) return launch_rows<Bf16Rows>(p, g.stream);
     return widens(g) ? launch_rows<Fp8WideRows>(p, g.stream) : launch_rows<Fp8Rows>(p, g.stream);
 }

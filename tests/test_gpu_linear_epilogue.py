@@ -239,6 +239,19 @@ def test_few_rows(q, axis, M, K, N, dtype, shard):
     np.testing.assert_array_equal(first, layer.run("none", True)[0])
 
 
+@pytest.mark.parametrize("q,axis,M,K,N", [(1, "y", 1, 512, 8), (1, "z", 15, 520, 136), (1, "y", 16, 4096, 128), (1, "y", 17, 2056, 264), (1, "z", 32, 2048, 1000),
+                                          (1, "y", 31, 6000, 392), (2, "y", 4, 528, 96), (2, "z", 28, 4112, 544), (3, "y", 9, 600, 72), (3, "z", 27, 2136, 648),
+                                          (4, "y", 16, 1056, 1152), (4, "z", 32, 2080, 256), (1, "y", 5, 20000, 256), (1, "z", 16, 504, 64)])
+@pytest.mark.parametrize("dist", ["int", "normal"])
+def test_few_rows_in_fp32(q, axis, M, K, N, dist):
+    layer = Layer(q, axis, M, K, N, "f32", dist, shard="f32")
+    for act, bias, residual, z in VARIANTS + [("gelu", True, "f32", "f32")]:
+        layer.check(act, bias, residual, z)
+    layer.check("relu", True, "f32", None, in_place=True)
+    first = layer.run("none", True)[0]
+    np.testing.assert_array_equal(first, layer.run("none", True)[0])
+
+
 # ---- the backward pass of the epilogue -------------------------------------------------------------
 
 def epilogue_bwd(q, axis, M, N, act, zt, gt, dt, dist="int", with_db=True, in_place=False):
