@@ -734,6 +734,8 @@ int virtual_cube_linear_fwd_fused(const cube3d_desc *desc, const cube3d_epilogue
     if (!X_shards || !W_shards || !Y_shards || misaligned(X_shards) || misaligned(W_shards) || misaligned(Y_shards) ||
         misaligned(epilogue->bias_diag))
         return CUBE3D_EINVAL;
+    for (const void *operand : {X_shards, W_shards})
+        if (operand == Y_shards || operand == epilogue->z) return CUBE3D_EINVAL;
     GemmMaps maps;
     GemmArgs a;
     rc = build_cube_product(desc, CUBE3D_OP_FWD, X_shards, W_shards, epilogue->bias_diag, Y_shards, stream, &maps, &a);

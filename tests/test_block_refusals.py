@@ -197,3 +197,8 @@ def test_norm_sizes_and_gradients_in_one_place(lib):
             g = b.NormParams(**{first: A, second: A})
             assert lib.virtual_cube_norm_bwd(ctypes.byref(matrix()), ctypes.byref(nd), ctypes.byref(NOTHING), E, X, N, R, U, Y, D,
                                              ctypes.byref(g), WS, 1 << 40, None) == c3.EINVAL
+
+
+def test_results_in_place_of_an_operand(lib):
+    for bad in (dict(y=X), dict(y=W), dict(z=X), dict(z=W), dict(z=X, z_dtype=c3.F32)):
+        assert fused(lib, **bad) == c3.EINVAL, bad
