@@ -37,7 +37,7 @@ class Stream:
 
 @pytest.fixture
 def two_devices(monkeypatch):
-    monkeypatch.setattr(b, "_one_device", lambda: False)
+    monkeypatch.setattr(b, "_one_device", False)
     monkeypatch.setattr(b, "_current_device", lambda: 0)
 
     def launched():
