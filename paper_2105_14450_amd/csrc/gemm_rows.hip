@@ -1,4 +1,5 @@
-// The forward product of few rows (tokens) with what follows it: Y = act(X W + b) + R for M <= 64 (fp32 32) over a cube of shards.
+// The forward product of few rows (tokens) with what follows it: Y = act(X W + b) + R over a cube of shards, for M up to 64 (fp32 32) and, in
+// blocks of that, to 512 (gemm_rows_plan says where).
 //
 // What bounds it: the weights, read once from HBM, M multiply-adds an element.  Nothing is shared between workgroups but X, so W goes
 // from memory straight to registers and into the matrix cores, without LDS, barriers or waits for other wavefronts, and
@@ -23,7 +24,8 @@ namespace cube3d {
 
 namespace {
 
-constexpr int COLS = 128, KSTEP = 32, WAVES = 4, MOST_ROWS = 64;
+constexpr int COLS = 128, KSTEP = 32, WAVES = 4;
+constexpr int most_rows_at_once(int64_t es) { return es == 4 ? 32 : 64; }
 
 struct RowsParams {
     const char *A, *B;
@@ -134,7 +136,7 @@ __device__ __forceinline__ void finish(const RowsParams &p, int m, int n, float 
     } else EpilogueRun<8>::apply_some(p.e, x, p.C, p.out_f32, row, p.maps.c_n, n, p.N);
 }
 
-// Grid: strips of 128 columns, runs of the contraction.
+// Grid: strips of 128 columns, runs of the contraction, blocks of 16 MT rows.
 template <typename E, int MT> __global__ __launch_bounds__(64 * WAVES, MT == (E::ELT == 4 ? 2 : 4) ? 1 : 2) void gemm_rows_kernel(const RowsParams p)
 {
     typedef typename E::Piece Piece;
@@ -142,7 +144,7 @@ template <typename E, int MT> __global__ __launch_bounds__(64 * WAVES, MT == (E:
     constexpr int PITCH = COLS + 4;
     __shared__ __attribute__((aligned(16))) float lds[WAVES][16 * PITCH];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), group = lane / 16, in_group = lane % 16;
-    const int n0 = blockIdx.x * COLS, split = blockIdx.y;
+    const int n0 = blockIdx.x * COLS, split = blockIdx.y, m0 = blockIdx.z * (16 * MT);
     const int first = (int)((int64_t)p.steps * split / p.splits), last = (int)((int64_t)p.steps * (split + 1) / p.splits);
     const char *b_row[8];
 #pragma unroll
@@ -150,7 +152,7 @@ template <typename E, int MT> __global__ __launch_bounds__(64 * WAVES, MT == (E:
     const unsigned b_col = (unsigned)(axis_offset_fast(p.maps.b_mn, min(n0 + 8 * in_group, p.N - 8)) * E::ELT);
     unsigned a_row[MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) a_row[t] = (unsigned)(axis_offset_fast(p.maps.a_mn, min(16 * t + in_group, p.M - 1)) * E::ELT);
+    for (int t = 0; t < MT; ++t) a_row[t] = (unsigned)(axis_offset_fast(p.maps.a_mn, min(m0 + 16 * t + in_group, p.M - 1)) * E::ELT);
 
     f32x4 acc[MT][8];
 #pragma unroll
@@ -210,7 +212,7 @@ template <typename E, int MT> __global__ __launch_bounds__(64 * WAVES, MT == (E:
                 *reinterpret_cast<f32x4 *>(&lds[wave][(4 * group + v) * PITCH + 8 * in_group + 4 * h]) =
                     f32x4{acc[t][4 * h][v], acc[t][4 * h + 1][v], acc[t][4 * h + 2][v], acc[t][4 * h + 3][v]};
         __syncthreads();
-        const int m = 16 * t + row, n = n0 + col;
+        const int m = m0 + 16 * t + row, n = n0 + col;
         if (m >= p.M || n >= p.N) continue;
         float s[8];
 #pragma unroll
@@ -255,7 +257,7 @@ bool eights(const AxisMap &m, int64_t extent, int64_t unit)
 
 template <typename E, int MT> int launch(const RowsParams &p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((p.N + COLS - 1) / COLS), (unsigned)p.splits);
+    const dim3 grid((unsigned)((p.N + COLS - 1) / COLS), (unsigned)p.splits, (unsigned)((p.M + 16 * MT - 1) / (16 * MT)));
     hipLaunchKernelGGL((gemm_rows_kernel<E, MT>), grid, dim3(64 * WAVES), 0, stream, p);
     if (const int rc = launch_status(); rc != CUBE3D_OK || p.splits == 1) return rc;
     const int64_t threads = (int64_t)p.M * (p.N / 8);
@@ -276,7 +278,7 @@ template <typename E> int launch_rows(const RowsParams &p, hipStream_t stream)
 int gemm_rows_plan(const GemmArgs &g)
 {
     if (!g.epilogue || !g.maps || g.batch != 1 || !g.a_kmajor || g.b_kmajor) return 0;
-    if (g.Mo > (g.in_dtype == CUBE3D_F32 ? MOST_ROWS / 2 : MOST_ROWS) || g.No >= 1ll << 24 || g.Kc >= 1ll << 30) return 0;
+    if (g.Mo > 512 || g.No >= 1ll << 24 || g.Kc >= 1ll << 30) return 0;
     const GemmMaps &m = *g.maps;
     const int64_t es = g.in_dtype == CUBE3D_F32 ? 4 : g.in_dtype == CUBE3D_BF16 ? 2 : 1;
     if (!eights(m.a_k, g.Kc, 1) || !eights(m.b_mn, g.No, 1) || !eights(m.b_k, g.Kc, m.b_k.u) || m.b_k.u % 8) return 0;
@@ -292,11 +294,20 @@ int gemm_rows_plan(const GemmArgs &g)
     // fp32, where the other kernels' one chain of K-tiles is longer: 512 x 512 7.8 / 9.1 (1 row), 8.6 / 9.3 (16); 2048 x 2048 11.8 / 19.3,
     // 13.0 / 19.6, 17.2 / 19.8 (32); 8192 x 2048 23 / 58, 24 / 58, 31 / 58; 8192 x 8192 56 / 66, 58 / 67; 32 rows, whose accumulators and
     // operands leave one wavefront a SIMD, 1024 x 4096 16.2 / 13.7, 2048 x 8192 28 / 23, 8192 x 8192 76 / 66
-    if (g.in_dtype == CUBE3D_F32) {
+    const int64_t at_once = most_rows_at_once(es), blocks = (g.Mo + at_once - 1) / at_once;
+    if (blocks > 1) {
+        // Several blocks of rows read the weights once each, from the caches if need be: where the ring's tiles of 64 leave half of the CUs
+        // without work for a long contraction.  bf16, here / there: 128 x 8192 x 2048 23 / 33, 256 x 8192 x 2048 31 / 44, 128 x 14336 x 4096
+        // 51 / 84, 512 x 24576 x 1024 67 / 126, 128 x 9216 x 1152 22.9 / 22.3, but 128 x 8192 x 8192 52 / 40, 512 x 8200 x 1544 74 / 53;
+        // fp8 128 x 16384 x 2048 30 / 48, 256 x 12000 x 1000 23.5 / 45, but 128 x 8192 x 2048 22 / 18; fp32 64 x 4096 x 1024 19 / 32,
+        // 128 x 16384 x 1024 59 / 108, but 192 x 9216 x 1152 70 / 65.
+        const int64_t tiles = ((g.Mo + 63) / 64) * ((g.No + 63) / 64);
+        if (tiles > (es == 4 ? 48 : 128) || g.Kc < (es == 4 ? 4096 : es == 2 ? 8192 : 10240)) return 0;
+    } else if (es == 4) {
         if (g.Kc < (g.Mo > 16 ? 2048 : 512) || (g.Mo > 16 && g.No > 4096)) return 0;
     } else if (g.Kc * es < 6144 || (g.Mo > 32 && g.No > 8192)) return 0;
     // As many runs as leave the busiest CU the fewest k-steps (20 KB per us and CU), against the traffic of their sums and a launch
-    const int64_t strips = (g.No + COLS - 1) / COLS, steps = (g.Kc + KSTEP - 1) / KSTEP, cus = num_compute_units();
+    const int64_t strips = (g.No + COLS - 1) / COLS * blocks, steps = (g.Kc + KSTEP - 1) / KSTEP, cus = num_compute_units();
     const double step_us = KSTEP * COLS * es / 20.3e3, run_us = (double)g.Mo * g.No * 8 / 5e6;
     int best = 1;
     double least = 0;

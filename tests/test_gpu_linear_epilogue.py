@@ -252,6 +252,21 @@ def test_few_rows_in_fp32(q, axis, M, K, N, dist):
     np.testing.assert_array_equal(first, layer.run("none", True)[0])
 
 
+# Blocks of rows, the last one of one row or whole, on runs of the contraction
+@pytest.mark.parametrize("q,axis,M,K,N,dtype", [(1, "y", 65, 10240, 136, "fp8_e4m3"), (1, "z", 127, 8200, 264, "bf16"), (1, "y", 128, 8192, 512, "bf16"),
+                                                (1, "y", 511, 10248, 200, "fp8_e4m3"), (1, "z", 512, 12288, 128, "bf16"), (2, "y", 132, 8208, 544, "bf16"),
+                                                (3, "z", 99, 10272, 72, "fp8_e4m3"), (4, "y", 144, 8320, 256, "bf16"), (1, "y", 33, 4096, 520, "f32"),
+                                                (2, "z", 96, 4112, 96, "f32"), (3, "y", 171, 4104, 72, "f32"), (1, "y", 512, 5000, 128, "f32")])
+def test_blocks_of_few_rows(q, axis, M, K, N, dtype):
+    layer = Layer(q, axis, M, K, N, dtype, shard="f32" if dtype == "f32" else "bf16")
+    assert c3.cube3d_epilogue_workspace_bytes(layer.desc, c3.OP_FWD) > 0, "not split"
+    for act, bias, residual, z in VARIANTS:
+        layer.check(act, bias, residual, z)
+    layer.check("relu", True, layer.shard, None, in_place=True)
+    first = layer.run("none", True)[0]
+    np.testing.assert_array_equal(first, layer.run("none", True)[0])
+
+
 # ---- the backward pass of the epilogue -------------------------------------------------------------
 
 def epilogue_bwd(q, axis, M, N, act, zt, gt, dt, dist="int", with_db=True, in_place=False):
