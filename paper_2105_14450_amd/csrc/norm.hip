@@ -20,7 +20,7 @@ constexpr int VECTORS = 5;      // post_gamma, post_beta, gate, pre_gamma, pre_b
 // ---- any size: one workgroup per row, the row read again for every step ---------------------------------
 // V consecutive columns at a time: eight where they lie side by side in every array, else four, two or one.  Bound by the
 // latency of narrow loads and of the passes over a row, of which a forward pass makes up to four: us, forward / backward,
-// 3000 x 4100 (four) 31 / 51, 20000 x 514 (two) 47 / 56, 3000 x 4101 (one) 68 / 85; in single elements the first was 69 / 84, the
+// 3000 x 4100 (four) 31 / 48, 20000 x 514 (two) 47 / 55, 3000 x 4101 (one) 68 / 83; in single elements the first was 69 / 84, the
 // second 94 / 97 (with four wavefronts a row).
 
 constexpr int ROW_LANES = 256;
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(LANES) void norm_bwd_rows_kernel(const NormArgs a, 
 // every fourth row, and leaves partial sums [group][vector][column].
 template <typename TS, typename TB, int V>
 __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a, const float *__restrict__ scalars, float *__restrict__ partials,
-                                                               int rows_per_group)
+                                                               int rows_per_group, int wanted)
 {
     __shared__ float lds[4][64 * V];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = (blockIdx.x * 64 + lane) * V;
@@ -289,7 +289,8 @@ __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a,
     if (!a.sums) return;
 #pragma unroll
     for (int v = 0; v < VECTORS; ++v) {
-        if (v > 0) __syncthreads();
+        if (!(wanted >> v & 1)) continue;
+        __syncthreads();
 #pragma unroll
         for (int e = 0; e < V; ++e) lds[wave][e * 64 + lane] = sum[v][e];
         __syncthreads();
@@ -522,7 +523,7 @@ template <typename TS, typename TB, int P> __global__ __launch_bounds__(1024) vo
 // Workgroup w leaves the sums over its rows in partials[w].  MOST: wavefronts of a workgroup (most_waves); with sixteen there are no
 // registers for both norms' parameters, which are read row by row then, and no row ahead.
 template <typename TS, typename TB, bool PRE, bool POST, int MOST>
-__global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, float *__restrict__ partials, int waves, int rows_at_once)
+__global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, float *__restrict__ partials, int waves, int rows_at_once, int wanted)
 {
     __shared__ float lds[2][2][16];
     extern __shared__ float tail[];      // rows_at_once > 1: their column sums, one vector at a time
@@ -648,8 +649,7 @@ __global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, f
     const int width = waves * 64 * VEC;
 #pragma unroll
     for (int v = 0; v < VECTORS; ++v) {
-        if (v < 2 && !POST) continue;
-        if (v > 2 && !PRE) continue;
+        if ((v < 2 && !POST) || (v > 2 && !PRE) || !(wanted >> v & 1)) continue;
         if (rows_at_once > 1) {
             __syncthreads();
 #pragma unroll
@@ -848,8 +848,8 @@ struct RowPlan {
 
 // Most wavefronts of a backward workgroup.  Both norms at once take some 150 registers a lane: twelve then (in sixteen they spill, or
 // do without what is read ahead), or eight where those hold whole rows and an fp32 stream takes more registers.  us with eight /
-// twelve, at 8192 rows with bf16 and with fp32 streams: 1024 columns 29.0 / 30.3, 31.7 / 34.4; 2048 45.5 / 44.0, 59.6 / 63.3;
-// 2560 81 / 59, 77 / 81; 6144 149 / 129 and 192 / 182 (sixteen / twelve).
+// twelve, at 8192 rows with bf16 and with fp32 streams: 1024 columns 28.0 / 28.4, 30.6 / 32.7; 2048 44.4 / 42.8, 57.7 / 60.8;
+// 2560 78 / 56, 76 / 79; 6144 147 / 127 and 190 / 179 (sixteen / twelve).
 int most_waves(const NormArgs &a, int waves)
 {
     if (a.pre_kind == CUBE3D_NORM_NONE || a.post_kind == CUBE3D_NORM_NONE || waves > 12) return 16;
@@ -866,7 +866,8 @@ RowPlan row_plan(const NormArgs &a, bool backward)
     const int64_t cus = num_compute_units();
     if (backward) {
         // A workgroup leaves a partial sum of every vector: as few of them as fill the CUs, of as many rows at once as that allows
-        // (2997 rows of 1152 with one norm, 62 MB: 45 us with 5 rows at once, 65 with one on five times as many workgroups)
+        // (one norm, us with several rows at once / one on as many more workgroups: 2997 x 1152 17.8 / 20.0, 8192 x 512 14.8 / 28.0,
+        // 32768 x 512 32.5 / 45.2, 8192 x 1024 20.8 / 26.8)
         const int fit = most_waves(a, p.waves) / p.waves;
         const int64_t each = (a.rows + cus - 1) / cus;
         p.rows_at_once = fit < each ? fit : (int)each;
@@ -989,7 +990,7 @@ int norm_bwd(const NormArgs &a, const cube3d_norm_params &gradients, void *works
                 constexpr bool PRE = decltype(pre_c)::value, POST = decltype(post_c)::value;
                 auto start = [&](auto most) {
                     hipLaunchKernelGGL((norm_bwd_kernel<TS, TB, PRE, POST, decltype(most)::value>), grid, block, lds, stream, a, partials,
-                                       plan.waves, plan.rows_at_once);
+                                       plan.waves, plan.rows_at_once, wanted);
                 };
                 if constexpr (PRE && POST) {
                     const int most = most_waves(a, plan.waves);
@@ -1020,7 +1021,7 @@ int norm_bwd(const NormArgs &a, const cube3d_norm_params &gradients, void *works
                 });
             if (const int e = launch_status(); e != CUBE3D_OK) return e;
             hipLaunchKernelGGL((norm_bwd_columns_kernel<TS, TB, V>), dim3((unsigned)((a.cols + 64 * V - 1) / (64 * V)), groups), dim3(256), 0,
-                               stream, a, scalars, partials, per);
+                               stream, a, scalars, partials, per, wanted);
             return launch_status();
         });
     });
