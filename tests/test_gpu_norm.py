@@ -185,6 +185,19 @@ def test_many_rows_and_long_ones(q, axis, rows, cols, post, pre):
     check_backward(pr)
 
 
+# four and two columns side by side, with one wavefront a row and with four, and workgroups of twelve wavefronts with several rows and with one
+WIDTHS = [(1, "y", 300, 4100), (1, "z", 640, 516), (2, "y", 304, 48), (1, "y", 3000, 514), (3, "z", 180, 630), (1, "y", 5, 16388), (2, "z", 100, 8200),
+          (1, "y", 1540, 1536), (1, "z", 1040, 2560), (1, "y", 300, 4608), (2, "y", 300, 6144)]
+
+
+@pytest.mark.parametrize("q,axis,rows,cols", WIDTHS)
+@pytest.mark.parametrize("stream,post,pre", [("bf16", "layer", "rms"), ("f32", "rms", "layer"), ("bf16", "none", "layer")])
+def test_widths_and_workgroups(q, axis, rows, cols, stream, post, pre):
+    pr = Problem(q, axis, rows, cols, stream, "bf16", post, pre)
+    check_forward(pr, *pr.forward())
+    check_backward(pr)
+
+
 @pytest.mark.parametrize("cols", [256, 129, 9000])
 def test_optional_parts(cols):
     """No parameters; no block (a norm alone); no residual gradient; single results; in place."""
