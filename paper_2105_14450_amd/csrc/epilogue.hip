@@ -69,7 +69,8 @@ __global__ __launch_bounds__(256) void epilogue_bwd_kernel(CubeGeom g, int RG, i
     }
 }
 
-int piece(const CubeGeom &g) { return g.Nb % VEC == 0 ? VEC : 1; }
+// Columns a lane owns: accesses of 16 bytes of bf16, or what the width of a block allows
+int piece(const CubeGeom &g) { return g.Nb % VEC == 0 ? VEC : g.Nb % 4 == 0 ? 4 : g.Nb % 2 == 0 ? 2 : 1; }
 
 // Lanes on a row, as a power of two
 int lane_shift(const CubeGeom &g)
@@ -120,12 +121,16 @@ int epilogue_bwd(const CubeGeom &g, int kind, int z_dtype, int dy_dtype, int dz_
         typedef decltype(td) TD;
         constexpr int KIND = decltype(kind_c)::value;
         float *part = dbias_diag ? workspace : nullptr;
-        if (V == VEC)
-            hipLaunchKernelGGL((epilogue_bwd_kernel<KIND, TZ, TG, TD, VEC>), grid, dim3(256), 0, stream, g, RG, NRG, shift,
+        auto of_width = [&](auto v) {
+            hipLaunchKernelGGL((epilogue_bwd_kernel<KIND, TZ, TG, TD, decltype(v)::value>), grid, dim3(256), 0, stream, g, RG, NRG, shift,
                                static_cast<const TZ *>(z), static_cast<const TG *>(dy), static_cast<TD *>(dz), part);
-        else
-            hipLaunchKernelGGL((epilogue_bwd_kernel<KIND, TZ, TG, TD, 1>), grid, dim3(256), 0, stream, g, RG, NRG, shift,
-                               static_cast<const TZ *>(z), static_cast<const TG *>(dy), static_cast<TD *>(dz), part);
+        };
+        switch (V) {
+        case VEC: of_width(std::integral_constant<int, VEC>{}); break;
+        case 4: of_width(std::integral_constant<int, 4>{}); break;
+        case 2: of_width(std::integral_constant<int, 2>{}); break;
+        default: of_width(std::integral_constant<int, 1>{});
+        }
         return launch_status();
     };
     const float f = 0.f;
