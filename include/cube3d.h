@@ -471,9 +471,9 @@ int virtual_cube_linear_epilogue_bwd(const cube3d_desc *desc, int kind, int z_dt
  *
  * Placement: `m` names a [rows, cols] matrix stored like activations: row_axis x, col_axis y or z, split by rows, that
  * is the X shards of a layer whose output direction is col_axis, or the Y shards of one whose input direction it
- * is; else CUBE3D_EINVAL.  q^2 must divide cols too; rows < 2^31, cols <= 2^31 - 2^16.  x, r (and dr, dx) are of m->dtype, u, n (du, dn) of
- * norm->block_dtype: F32 or BF16.  Every vector is fp32 in diagonal storage, as virtual_cube_scatter(desc,
- * CUBE3D_OPERAND_BIAS) of a layer of N = cols makes it.
+ * is; else CUBE3D_EINVAL.  q^2 must divide cols too; rows < 2^31, cols <= 2^31 - 2^16.  x, r (and dr, dx) are of
+ * m->dtype, u, n (du, dn) of norm->block_dtype: F32 or BF16.  Every vector is fp32 in diagonal storage, as
+ * virtual_cube_scatter(desc, CUBE3D_OPERAND_BIAS) of a layer of N = cols makes it.
  *   parameters    post_gamma, post_beta belong to Npost, pre_gamma, pre_beta to Npre; NULL: gamma = 1, beta = 0,
  *                 g = 1.  Ignored where the kind is NONE.
  *   u             NULL: r = x (nothing written: r must be NULL) and n = Npre(x); post_kind must be NONE.
@@ -487,10 +487,11 @@ int virtual_cube_linear_epilogue_bwd(const cube3d_desc *desc, int kind, int z_dt
  *     Dr = dr + Npre'(dn),  dx = Dr,  du = Npost'(scale * g * Dr)
  * and the gradients of the parameters as column sums over all rows in fp32, in a fixed order (those of Npre from dn, of
  * Npost and g from Dr in fp32), written to the vectors of `gradients` that are not NULL (no two the same), in diagonal
- * storage (entries off the diagonal written as zero).  r is the stored stream behind the block (read if pre_kind is not NONE; the
- * stream x itself where the forward pass had no u), u the block's output (read if post_kind is not NONE or the gate's gradient is asked for), stats the
- * forward pass's.  dn is NULL exactly if pre_kind is NONE; dx may be NULL (not written), and so may du; one of dr and dn and
- * one of the results must be there; without u (NULL) du, post_kind and the gradients of gate and Npost must be absent.  dx may be dr itself.
+ * storage (entries off the diagonal written as zero).  r is the stored stream behind the block (read if pre_kind is not
+ * NONE; the stream x itself where the forward pass had no u), u the block's output (read if post_kind is not NONE or the
+ * gate's gradient is asked for), stats the forward pass's.  dn is NULL exactly if pre_kind is NONE; dx may be NULL (not
+ * written), and so may du; one of dr and dn and one of the results must be there; without u (NULL) du, post_kind and the
+ * gradients of gate and Npost must be absent.  dx may be dr itself.
  * `workspace`: at least cube3d_norm_workspace_bytes(m, norm) bytes of device scratch, 16-byte aligned, else
  * CUBE3D_EWORKSPACE.
  */
