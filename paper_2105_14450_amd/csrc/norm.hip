@@ -18,10 +18,8 @@ namespace {
 constexpr int VECTORS = 5;      // post_gamma, post_beta, gate, pre_gamma, pre_beta
 
 // ---- any size: one workgroup per row, the row read again for every step ---------------------------------
-// V consecutive columns at a time: eight where they lie side by side in every array, else four, two or one.  Bound by the
-// latency of narrow loads and of the passes over a row, of which a forward pass makes up to four: us, forward / backward,
-// 3000 x 4100 (four) 31 / 48, 20000 x 514 (two) 47 / 55, 3000 x 4101 (one) 68 / 83; in single elements the first was 69 / 84, the
-// second 94 / 97 (with four wavefronts a row).
+// For what registers do not hold.  V consecutive columns at a time: eight where they lie side by side in every array, else four, two or
+// one.  Bound by the latency of narrow loads and of the passes over a row, of which a forward pass makes up to four.
 
 constexpr int ROW_LANES = 256;
 
@@ -338,10 +336,16 @@ __global__ __launch_bounds__(64 * FINISH_WAVES) void norm_bwd_finish_kernel(cons
 }
 
 // ---- rows in registers ----------------------------------------------------------------------------------
-// Where eight consecutive columns lie side by side in every array (blocks and vector shards of a multiple of eight columns), a row is held
-// by `waves` wavefronts, eight columns times P a lane, and read once; short rows share a workgroup.  A lane keeps its columns from
-// row to row: offsets and parameters are looked up once, the backward pass's column sums grow in registers, and the next row is
-// on its way while the last one's sums are formed.
+// A row is held by `waves` wavefronts, eight columns times P a lane, and read once; short rows share a workgroup.  A lane keeps its
+// columns from row to row: offsets and parameters are looked up once, the backward pass's column sums grow in registers, and the
+// next row is on its way while the last one's sums are formed.
+//
+// Where eight consecutive columns lie side by side and aligned in every array (blocks and vector shards of a multiple of eight
+// columns) every lane has eight.  Else (RAGGED) each vector shard is cut into runs of eight and a last one of what is left; whole runs
+// still move in 16-byte accesses, which need no alignment.  us, forward / backward, here and in narrow accesses as above:
+// 3000 x 4101 34 / 48 and 68 / 83, 20000 x 514 29 / 47 and 48 / 54, 3000 x 4001 with both norms and an fp32 stream 45 / 66 and
+// 143 / 122, 32768 x 516 (q = 2) 64 / 139 and 274 / 288.  Runs of four are as fast there (3000 x 4100 31 / 48) and stay, and so does the
+// backward pass of both norms with more than eight wavefronts a row (4000 x 6001: 395 us here with spills, 328).
 //
 // What bounds it: HBM.  TB/s of necessary bytes, forward / backward, a copy of 1 GiB making 4.8: 32768 x 8192 bf16 5.0 / 5.1;
 // 8192 x 2048 (200 MB, in part from the Infinity Cache) 5.8 / 4.9; 16384 x 8192 with both norms and an fp32 stream 5.1 / 5.0;
@@ -399,7 +403,56 @@ template <typename T> __device__ __forceinline__ void unpack(const Pack8<T> &v, 
     for (int e = 0; e < VEC; ++e) x[e] = to_f32<T>(v.v[e]);
 }
 
-template <typename TS, typename TB, int P> __global__ __launch_bounds__(1024) void norm_fwd_kernel(const NormArgs a, int waves, int rows_at_once)
+// Where a lane's columns begin, and how many there are: eight (0 beyond the row's end), or, RAGGED, eight of a vector's shard of Cs
+// columns or what is left of it.  (Runs of a shard lie side by side in every array, at any alignment.)
+struct Run {
+    int c, valid;
+};
+template <bool RAGGED> __device__ __forceinline__ Run run_of(const NormArgs &a, int number)
+{
+    if constexpr (!RAGGED) return Run{number * VEC, number * VEC < a.cols ? VEC : 0};
+    const int Cs = a.vec.P2, runs = (Cs + VEC - 1) / VEC, shard = number / runs, at = (number - shard * runs) * VEC;
+    return Run{shard * Cs + at, shard < a.q * a.q ? min(Cs - at, VEC) : 0};
+}
+
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Loose8 {
+    T v[VEC];
+};
+template <bool RAGGED, typename T> __device__ __forceinline__ Pack8<T> get_run(const T *from, int valid)
+{
+    if constexpr (!RAGGED) return *reinterpret_cast<const Pack8<T> *>(from);
+    if (valid == VEC) return __builtin_bit_cast(Pack8<T>, *reinterpret_cast<const Loose8<T> *>(from));
+    Pack8<T> x;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x.v[e] = e < valid ? from[e] : T(0);
+    return x;
+}
+template <bool RAGGED, typename T> __device__ __forceinline__ void put_run(T *to, int valid, const Pack8<T> &x)
+{
+    if constexpr (!RAGGED) {
+        *reinterpret_cast<Pack8<T> *>(to) = x;
+        return;
+    }
+    if (valid == VEC) {
+        *reinterpret_cast<Loose8<T> *>(to) = __builtin_bit_cast(Loose8<T>, x);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+        if (e < valid) to[e] = x.v[e];
+}
+template <bool RAGGED> __device__ __forceinline__ void vector_run(const float *v, int64_t at, int valid, float absent, float (&x)[VEC])
+{
+    if constexpr (!RAGGED) {
+        vector_at<VEC>(v, at, absent, x);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) x[e] = v && e < valid ? v[at + e] : absent;
+}
+
+template <typename TS, typename TB, int P, bool RAGGED>
+__global__ __launch_bounds__(1024) void norm_fwd_kernel(const NormArgs a, int waves, int rows_at_once)
 {
     __shared__ float lds[2][2][16];
     RowGroup g;
@@ -417,6 +470,7 @@ template <typename TS, typename TB, int P> __global__ __launch_bounds__(1024) vo
     const bool post = a.post_kind != CUBE3D_NORM_NONE, pre = a.pre_kind != CUBE3D_NORM_NONE;
     const float inv = 1.f / (float)a.cols;
     int64_t col[P];
+    int valid[P];
     bool live[P];
     // (two pieces a lane leave no registers for the parameters: those are read row by row)
     constexpr bool HELD = P == 1;
@@ -424,20 +478,21 @@ template <typename TS, typename TB, int P> __global__ __launch_bounds__(1024) vo
     int64_t vec[P];
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        const int c = ((p * waves + g.wave - g.first) * 64 + g.lane) * VEC;
-        live[p] = c < a.cols;
-        const int cc = live[p] ? c : 0;
+        const Run run = run_of<RAGGED>(a, (p * waves + g.wave - g.first) * 64 + g.lane);
+        valid[p] = run.valid;
+        live[p] = run.valid > 0;
+        const int cc = live[p] ? run.c : 0;
         col[p] = axis_offset_fast(a.col, cc);
         vec[p] = axis_offset_fast(a.vec, cc);
     }
     auto look_up_post = [&](int p) {
-        vector_at<VEC>(a.p.post_gamma, vec[p], 1.f, post_gamma);
-        vector_at<VEC>(a.p.post_beta, vec[p], 0.f, post_beta);
+        vector_run<RAGGED>(a.p.post_gamma, vec[p], valid[p], 1.f, post_gamma);
+        vector_run<RAGGED>(a.p.post_beta, vec[p], valid[p], 0.f, post_beta);
     };
-    auto look_up_gate = [&](int p) { vector_at<VEC>(a.p.gate, vec[p], 1.f, gate); };
+    auto look_up_gate = [&](int p) { vector_run<RAGGED>(a.p.gate, vec[p], valid[p], 1.f, gate); };
     auto look_up_pre = [&](int p) {
-        vector_at<VEC>(a.p.pre_gamma, vec[p], 1.f, pre_gamma);
-        vector_at<VEC>(a.p.pre_beta, vec[p], 0.f, pre_beta);
+        vector_run<RAGGED>(a.p.pre_gamma, vec[p], valid[p], 1.f, pre_gamma);
+        vector_run<RAGGED>(a.p.pre_beta, vec[p], valid[p], 0.f, pre_beta);
     };
     if constexpr (HELD) {
         look_up_post(0);
@@ -451,8 +506,8 @@ template <typename TS, typename TB, int P> __global__ __launch_bounds__(1024) vo
         const int64_t at = axis_offset_fast(a.row, min(row, a.rows - 1));
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-            xr[p] = *reinterpret_cast<const Pack8<TS> *>(x + at + col[p]);
-            if (a.u) ur[p] = *reinterpret_cast<const Pack8<TB> *>(u + at + col[p]);
+            xr[p] = get_run<RAGGED>(x + at + col[p], valid[p]);
+            if (a.u) ur[p] = get_run<RAGGED>(u + at + col[p], valid[p]);
         }
     };
     // sum over the row of f(piece, element), lanes beyond its end aside
@@ -461,7 +516,7 @@ template <typename TS, typename TB, int P> __global__ __launch_bounds__(1024) vo
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) s[0] += live[p] ? f(p, e) : 0.f;
+            for (int e = 0; e < VEC; ++e) s[0] += (RAGGED ? e < valid[p] : live[p]) ? f(p, e) : 0.f;
         group_sum<1>(g, s);
         return s[0];
     };
@@ -506,13 +561,13 @@ template <typename TS, typename TB, int P> __global__ __launch_bounds__(1024) vo
 #pragma unroll
         for (int p = 0; p < P; ++p) {
             if (!live[p]) continue;
-            if (r_out) *reinterpret_cast<Pack8<TS> *>(r_out + at + col[p]) = pack_out<TS>(r[p]);
+            if (r_out) put_run<RAGGED>(r_out + at + col[p], valid[p], pack_out<TS>(r[p]));
             if (pre) {
                 if constexpr (!HELD) look_up_pre(p);
                 float n[VEC];
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) n[e] = (r[p][e] - pre_mean) * pre_rstd * pre_gamma[e] + pre_beta[e];
-                *reinterpret_cast<Pack8<TB> *>(n_out + at + col[p]) = pack_out<TB>(n);
+                put_run<RAGGED>(n_out + at + col[p], valid[p], pack_out<TB>(n));
             }
         }
         if (a.stats_out && g.wave == g.first && g.lane == 0)
@@ -522,7 +577,7 @@ template <typename TS, typename TB, int P> __global__ __launch_bounds__(1024) vo
 
 // Workgroup w leaves the sums over its rows in partials[w].  MOST: wavefronts of a workgroup (most_waves); with sixteen there are no
 // registers for both norms' parameters, which are read row by row then, and no row ahead.
-template <typename TS, typename TB, bool PRE, bool POST, int MOST>
+template <typename TS, typename TB, bool PRE, bool POST, int MOST, bool RAGGED>
 __global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, float *__restrict__ partials, int waves, int rows_at_once, int wanted)
 {
     __shared__ float lds[2][2][16];
@@ -540,17 +595,19 @@ __global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, f
     TS *dx = static_cast<TS *>(a.dx);
     TB *du = static_cast<TB *>(a.du);
     const float inv = 1.f / (float)a.cols;
-    const int own = (g.wave - g.first) * 64 + g.lane, c = own * VEC;
-    const bool live = c < a.cols;
+    const int own = (g.wave - g.first) * 64 + g.lane;
+    const Run run = run_of<RAGGED>(a, own);
+    const int c = run.c, valid = run.valid;
+    const bool live = valid > 0;
     const int64_t col = axis_offset_fast(a.col, live ? c : 0), vec = axis_offset_fast(a.vec, live ? c : 0);
     float post_gamma[VEC], post_beta[VEC], gate[VEC], pre_gamma[VEC];
     constexpr bool HELD = !(PRE && POST && MOST == 16);
-    auto look_up_pre = [&]() { vector_at<VEC>(a.p.pre_gamma, vec, 1.f, pre_gamma); };
+    auto look_up_pre = [&]() { vector_run<RAGGED>(a.p.pre_gamma, vec, valid, 1.f, pre_gamma); };
     auto look_up_post = [&]() {
-        vector_at<VEC>(a.p.gate, vec, 1.f, gate);
+        vector_run<RAGGED>(a.p.gate, vec, valid, 1.f, gate);
         if constexpr (POST) {
-            vector_at<VEC>(a.p.post_gamma, vec, 1.f, post_gamma);
-            vector_at<VEC>(a.p.post_beta, vec, 0.f, post_beta);
+            vector_run<RAGGED>(a.p.post_gamma, vec, valid, 1.f, post_gamma);
+            vector_run<RAGGED>(a.p.post_beta, vec, valid, 0.f, post_beta);
         }
     };
     if constexpr (HELD) {
@@ -568,12 +625,12 @@ __global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, f
     const bool with_u = POST || a.read_u;
     auto load = [&](int64_t row) {
         const int64_t rr = min(row, a.rows - 1), at = axis_offset_fast(a.row, rr) + col;
-        if (dr) dr_raw = *reinterpret_cast<const Pack8<TS> *>(dr + at);
+        if (dr) dr_raw = get_run<RAGGED>(dr + at, valid);
         if constexpr (PRE) {
-            dn_raw = *reinterpret_cast<const Pack8<TB> *>(dn + at);
-            r_raw = *reinterpret_cast<const Pack8<TS> *>(r + at);
+            dn_raw = get_run<RAGGED>(dn + at, valid);
+            r_raw = get_run<RAGGED>(r + at, valid);
         }
-        if (with_u) u_raw = *reinterpret_cast<const Pack8<TB> *>(u + at);
+        if (with_u) u_raw = get_run<RAGGED>(u + at, valid);
         if constexpr (PRE || POST) st_raw = *reinterpret_cast<const f32x4 *>(a.stats + 4 * rr);
     };
     const int64_t step = (int64_t)gridDim.x * rows_at_once;
@@ -581,6 +638,7 @@ __global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, f
     load(row);
     for (int64_t base = (int64_t)blockIdx.x * rows_at_once; base < a.rows; base += step, row += step) {
         const bool here = live && row < a.rows;
+        auto ok = [&](int e) { return RAGGED ? here && e < valid : here; };
         float d[VEC], t[VEC], hat[VEC], w[VEC];
         f32x4 st;
         if (dr) unpack(dr_raw, d);
@@ -601,27 +659,27 @@ __global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, f
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
                 hat[e] = (hat[e] - st[2]) * st[3];
-                const float b = here ? t[e] : 0.f;
-                sum[3][e] = fmaf(b, here ? hat[e] : 0.f, sum[3][e]);
+                const float b = ok(e) ? t[e] : 0.f;
+                sum[3][e] = fmaf(b, ok(e) ? hat[e] : 0.f, sum[3][e]);
                 sum[4][e] += b;
-                t[e] = here ? t[e] * pre_gamma[e] : 0.f;
+                t[e] = ok(e) ? t[e] * pre_gamma[e] : 0.f;
                 m[0] += t[e];
-                m[1] = fmaf(t[e], here ? hat[e] : 0.f, m[1]);
+                m[1] = fmaf(t[e], ok(e) ? hat[e] : 0.f, m[1]);
             }
             group_sum<2>(g, m);
             const float m0 = a.pre_kind == CUBE3D_NORM_LAYER ? m[0] * inv : 0.f, m1 = m[1] * inv;
 #pragma unroll
             for (int e = 0; e < VEC; ++e) d[e] += st[3] * (t[e] - m0 - hat[e] * m1);
         }
-        if (dx && here) *reinterpret_cast<Pack8<TS> *>(dx + at) = pack_out<TS>(d);
+        if (dx && here) put_run<RAGGED>(dx + at, valid, pack_out<TS>(d));
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) d[e] = here ? d[e] * a.scale : 0.f;
+        for (int e = 0; e < VEC; ++e) d[e] = ok(e) ? d[e] * a.scale : 0.f;
         if constexpr (!HELD) look_up_post();
         if constexpr (POST) {
             float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                w[e] = here ? (w[e] - st[0]) * st[1] : 0.f;
+                w[e] = ok(e) ? (w[e] - st[0]) * st[1] : 0.f;
                 sum[2][e] = fmaf(d[e], w[e] * post_gamma[e] + post_beta[e], sum[2][e]);
                 d[e] *= gate[e];
                 sum[0][e] = fmaf(d[e], w[e], sum[0][e]);
@@ -637,11 +695,11 @@ __global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, f
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                if (with_u) sum[2][e] = fmaf(d[e], here ? w[e] : 0.f, sum[2][e]);
+                if (with_u) sum[2][e] = fmaf(d[e], ok(e) ? w[e] : 0.f, sum[2][e]);
                 d[e] *= gate[e];
             }
         }
-        if (du && here) *reinterpret_cast<Pack8<TB> *>(du + at) = pack_out<TB>(d);
+        if (du && here) put_run<RAGGED>(du + at, valid, pack_out<TB>(d));
         if (!HELD && base + step < a.rows) load(row + step);
     }
     if (!a.sums) return;
@@ -660,7 +718,11 @@ __global__ __launch_bounds__(64 * MOST) void norm_bwd_kernel(const NormArgs a, f
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) sum[v][e] += tail[k * width + e * waves * 64 + own];
         }
-        if (group == 0 && live) {
+        if (RAGGED && group == 0) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (e < valid) out[(int64_t)v * a.cols + c + e] = sum[v][e];
+        } else if (group == 0 && live) {
             f32x4 *dst = reinterpret_cast<f32x4 *>(out + (int64_t)v * a.cols + c);
             dst[0] = f32x4{sum[v][0], sum[v][1], sum[v][2], sum[v][3]};
             dst[1] = f32x4{sum[v][4], sum[v][5], sum[v][6], sum[v][7]};
@@ -839,36 +901,47 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(const NormArgs a, f
             }
 }
 
-// How rows are dealt out: wavefronts per row, rows per workgroup, pieces of eight columns per lane, workgroups; waves = 0: the row does not
-// fit, or does not lie in eights.
+// How rows are dealt out: wavefronts per row, rows per workgroup, pieces of eight columns per lane, workgroups, whether runs are ragged;
+// waves = 0: not in registers.
 struct RowPlan {
     int waves, rows_at_once, pieces;
     unsigned groups;
+    bool ragged;
 };
 
 // Most wavefronts of a backward workgroup.  Both norms at once take some 150 registers a lane: twelve then (in sixteen they spill, or
 // do without what is read ahead), or eight where those hold whole rows and an fp32 stream takes more registers.  us with eight /
 // twelve, at 8192 rows with bf16 and with fp32 streams: 1024 columns 28.0 / 28.4, 30.6 / 32.7; 2048 44.4 / 42.8, 57.7 / 60.8;
 // 2560 78 / 56, 76 / 79; 6144 147 / 127 and 190 / 179 (sixteen / twelve).
-int most_waves(const NormArgs &a, int waves)
+// (Ragged runs take a few registers more: one size less.  Sixteen wavefronts of one norm spill 12 to 17 registers and still are
+// faster than the any-size kernels: 3000 x 8001 80 us for 150.)
+int most_waves(const NormArgs &a, int waves, bool ragged)
 {
-    if (a.pre_kind == CUBE3D_NORM_NONE || a.post_kind == CUBE3D_NORM_NONE || waves > 12) return 16;
+    const bool both = a.pre_kind != CUBE3D_NORM_NONE && a.post_kind != CUBE3D_NORM_NONE;
+    if (ragged) return both ? 8 : waves <= 12 ? 12 : 16;
+    if (!both || waves > 12) return 16;
     return waves <= 2 || (waves <= 8 && a.stream_f32) ? 8 : 12;
 }
 
 RowPlan row_plan(const NormArgs &a, bool backward)
 {
-    RowPlan p{0, 1, 1, 0};
-    if (widest(a) != VEC) return p;
-    if (a.cols > 32 * SHORT_ROW) return p;
-    p.pieces = a.cols > 16 * SHORT_ROW ? 2 : 1;
-    p.waves = (a.cols + SHORT_ROW * p.pieces - 1) / (SHORT_ROW * p.pieces);
+    const int width = widest(a);
+    RowPlan p{0, 1, 1, 0, width != VEC};
+    if (width == VEC / 2) return p;
+    const int64_t runs = p.ragged ? (int64_t)a.q * a.q * ((a.vec.P2 + VEC - 1) / VEC) : a.cols / VEC, most = SHORT_ROW / VEC;
+    if (runs > (p.ragged ? 16 : 32) * most) return p;
+    p.pieces = runs > 16 * most ? 2 : 1;
+    p.waves = (int)((runs + most * p.pieces - 1) / (most * p.pieces));
+    if (backward && p.ragged && p.waves > most_waves(a, p.waves, true)) {
+        p.waves = 0;
+        return p;
+    }
     const int64_t cus = num_compute_units();
     if (backward) {
         // A workgroup leaves a partial sum of every vector: as few of them as fill the CUs, of as many rows at once as that allows
         // (one norm, us with several rows at once / one on as many more workgroups: 2997 x 1152 17.8 / 20.0, 8192 x 512 14.8 / 28.0,
         // 32768 x 512 32.5 / 45.2, 8192 x 1024 20.8 / 26.8)
-        const int fit = most_waves(a, p.waves) / p.waves;
+        const int fit = most_waves(a, p.waves, p.ragged) / p.waves;
         const int64_t each = (a.rows + cus - 1) / cus;
         p.rows_at_once = fit < each ? fit : (int)each;
     } else p.rows_at_once = p.waves == 1 ? 4 : p.waves == 2 ? 2 : 1;
@@ -926,10 +999,12 @@ int norm_fwd(const NormArgs &a, hipStream_t stream)
                 });
                 return launch_status();
             });
-        if (plan.pieces == 1)
-            hipLaunchKernelGGL((norm_fwd_kernel<TS, TB, 1>), dim3(plan.groups), block, 0, stream, a, plan.waves, plan.rows_at_once);
+        if (plan.ragged)
+            hipLaunchKernelGGL((norm_fwd_kernel<TS, TB, 1, true>), dim3(plan.groups), block, 0, stream, a, plan.waves, plan.rows_at_once);
+        else if (plan.pieces == 1)
+            hipLaunchKernelGGL((norm_fwd_kernel<TS, TB, 1, false>), dim3(plan.groups), block, 0, stream, a, plan.waves, plan.rows_at_once);
         else
-            hipLaunchKernelGGL((norm_fwd_kernel<TS, TB, 2>), dim3(plan.groups), block, 0, stream, a, plan.waves, plan.rows_at_once);
+            hipLaunchKernelGGL((norm_fwd_kernel<TS, TB, 2, false>), dim3(plan.groups), block, 0, stream, a, plan.waves, plan.rows_at_once);
         return launch_status();
     });
 }
@@ -988,16 +1063,22 @@ int norm_bwd(const NormArgs &a, const cube3d_norm_params &gradients, void *works
             typedef decltype(b) TB;
             auto launch = [&](auto pre_c, auto post_c) {
                 constexpr bool PRE = decltype(pre_c)::value, POST = decltype(post_c)::value;
-                auto start = [&](auto most) {
-                    hipLaunchKernelGGL((norm_bwd_kernel<TS, TB, PRE, POST, decltype(most)::value>), grid, block, lds, stream, a, partials,
-                                       plan.waves, plan.rows_at_once, wanted);
+                auto start = [&](auto most, auto ragged) {
+                    hipLaunchKernelGGL((norm_bwd_kernel<TS, TB, PRE, POST, decltype(most)::value, decltype(ragged)::value>), grid, block, lds,
+                                       stream, a, partials, plan.waves, plan.rows_at_once, wanted);
                 };
+                const std::integral_constant<int, 8> eight{};
+                const std::integral_constant<int, 12> twelve{};
+                const std::integral_constant<int, 16> sixteen{};
+                const std::true_type ragged{};
+                const std::false_type whole{};
+                const int most = most_waves(a, plan.waves, plan.ragged);
                 if constexpr (PRE && POST) {
-                    const int most = most_waves(a, plan.waves);
-                    if (most == 8) start(std::integral_constant<int, 8>{});
-                    else if (most == 12) start(std::integral_constant<int, 12>{});
-                    else start(std::integral_constant<int, 16>{});
-                } else start(std::integral_constant<int, 16>{});
+                    if (plan.ragged) start(eight, ragged);
+                    else if (most == 8) start(eight, whole);
+                    else most == 12 ? start(twelve, whole) : start(sixteen, whole);
+                } else if (plan.ragged) most == 12 ? start(twelve, ragged) : start(sixteen, ragged);
+                else start(sixteen, whole);
                 return launch_status();
             };
             const std::true_type yes{};

@@ -198,6 +198,19 @@ def test_widths_and_workgroups(q, axis, rows, cols, stream, post, pre):
     check_backward(pr)
 
 
+# shards of odd sizes: runs of eight columns and what is left, one column to whole workgroups
+RAGGED = [(1, "y", 300, 4101), (1, "z", 64, 8001), (2, "y", 400, 516), (1, "y", 600, 2503), (3, "z", 90, 1143), (1, "z", 1100, 129), (1, "y", 40, 6001),
+          (3, "y", 2700, 27), (2, "z", 1200, 4), (1, "y", 5000, 9), (1, "z", 30, 8193), (4, "y", 64, 2064), (5, "z", 50, 275)]
+
+
+@pytest.mark.parametrize("q,axis,rows,cols", RAGGED)
+@pytest.mark.parametrize("stream,post,pre", [("bf16", "layer", "rms"), ("f32", "rms", "layer"), ("bf16", "none", "layer"), ("f32", "layer", "none")])
+def test_shards_of_odd_sizes(q, axis, rows, cols, stream, post, pre):
+    pr = Problem(q, axis, rows, cols, stream, "bf16", post, pre)
+    check_forward(pr, *pr.forward())
+    check_backward(pr)
+
+
 @pytest.mark.parametrize("cols", [256, 129, 9000])
 def test_optional_parts(cols):
     """No parameters; no block (a norm alone); no residual gradient; single results; in place."""
