@@ -17,8 +17,38 @@ template <typename T, int V> struct __attribute__((aligned(sizeof(T) * V))) Run 
     T v[V];
 };
 
+template <typename To, typename From> __device__ __forceinline__ To bit_cast_to(const From &x) { return __builtin_bit_cast(To, x); }
+
+// V elements at any alignment, or the first `valid` of them
+template <typename T, int V> struct __attribute__((packed, aligned(sizeof(T)))) LooseRun {
+    T v[V];
+};
+template <bool LOOSE, typename T, int V> __device__ __forceinline__ Run<T, V> get_run(const T *from, int valid)
+{
+    if constexpr (!LOOSE) return *reinterpret_cast<const Run<T, V> *>(from);
+    if (valid == V) return bit_cast_to<Run<T, V>>(*reinterpret_cast<const LooseRun<T, V> *>(from));
+    Run<T, V> x;
+#pragma unroll
+    for (int e = 0; e < V; ++e) x.v[e] = e < valid ? from[e] : T(0);
+    return x;
+}
+template <bool LOOSE, typename T, int V> __device__ __forceinline__ void put_run(T *to, int valid, const Run<T, V> &x)
+{
+    if constexpr (!LOOSE) {
+        *reinterpret_cast<Run<T, V> *>(to) = x;
+        return;
+    }
+    if (valid == V) {
+        *reinterpret_cast<LooseRun<T, V> *>(to) = bit_cast_to<LooseRun<T, V>>(x);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (e < valid) to[e] = x.v[e];
+}
+
 // Grid: chunks of 2^shift lanes' columns, row groups, processors.  A wavefront takes 64 / 2^shift rows at a time (narrow blocks: several).
-template <int KIND, typename TZ, typename TG, typename TD, int V>
+template <int KIND, typename TZ, typename TG, typename TD, int V, bool LOOSE>
 __global__ __launch_bounds__(256) void epilogue_bwd_kernel(CubeGeom g, int RG, int NRG, int shift, const TZ *z, const TG *dy, TD *dz,
                                                            float *__restrict__ part)
 {
@@ -26,7 +56,8 @@ __global__ __launch_bounds__(256) void epilogue_bwd_kernel(CubeGeom g, int RG, i
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int r = blockIdx.z, rg = blockIdx.y, width = 1 << shift, rows = 64 >> shift;
     const int64_t c0 = ((int64_t)blockIdx.x * width + (lane & (width - 1))) * V;
-    const bool live = c0 < g.Nb;                       // Nb % V == 0: a lane is all in or all out
+    const bool live = c0 < g.Nb;                       // (Nb % V == 0: a lane is all in or all out)
+    const int valid = LOOSE ? (int)min((int64_t)V, g.Nb - c0) : V;
     const int64_t row_lo = (int64_t)rg * RG, row_hi = row_lo + RG < g.Ms ? row_lo + RG : g.Ms;
     const int64_t t_lo = row_lo + wave * rows + (lane >> shift), step = (int64_t)(4 * rows) * g.Nb;      // elements between a lane's rows
     int64_t at = ((int64_t)r * g.Ms + t_lo) * g.Nb + c0;
@@ -35,8 +66,8 @@ __global__ __launch_bounds__(256) void epilogue_bwd_kernel(CubeGeom g, int RG, i
     for (int e = 0; e < V; ++e) acc[e] = 0.f;
     const int turns = live && t_lo < row_hi ? (int)((row_hi - t_lo + 4 * rows - 1) / (4 * rows)) : 0;
     for (int n = 0; n < turns; ++n, at += step) {      // (two and four rows at a time: 94.7 and 95.3 us for 91.0 at 8192 x 8192 bf16)
-        const Run<TZ, V> zv = *reinterpret_cast<const Run<TZ, V> *>(z + at);
-        const Run<TG, V> gv = *reinterpret_cast<const Run<TG, V> *>(dy + at);
+        const Run<TZ, V> zv = get_run<LOOSE, TZ, V>(z + at, valid);
+        const Run<TG, V> gv = get_run<LOOSE, TG, V>(dy + at, valid);
         Run<TD, V> o;
         float x[V];
 #pragma unroll
@@ -51,7 +82,7 @@ __global__ __launch_bounds__(256) void epilogue_bwd_kernel(CubeGeom g, int RG, i
 #pragma unroll
             for (int e = 0; e < V; ++e) o.v[e] = from_f32<TD>(x[e]);
         }
-        *reinterpret_cast<Run<TD, V> *>(dz + at) = o;
+        put_run<LOOSE, TD, V>(dz + at, valid, o);
     }
     if (part == nullptr) return;
 #pragma unroll
@@ -69,8 +100,13 @@ __global__ __launch_bounds__(256) void epilogue_bwd_kernel(CubeGeom g, int RG, i
     }
 }
 
-// Columns a lane owns: accesses of 16 bytes of bf16, or what the width of a block allows
-int piece(const CubeGeom &g) { return g.Nb % VEC == 0 ? VEC : g.Nb % 4 == 0 ? 4 : g.Nb % 2 == 0 ? 2 : 1; }
+// Columns a lane owns: eight, or four or two where that is what blocks are a multiple of.  Long odd blocks: eight in accesses of any
+// alignment, the last lane of a row what is left (us, in eights / single elements: 8192 x 4101 bf16 51 / 80, fp32 110 / 126; but
+// 30000 x 129 30 / 23; in twos, 8192 x 4098 bf16 49 / 52, fp32 111 / 93)
+int piece(const CubeGeom &g)
+{
+    return g.Nb % VEC == 0 ? VEC : g.Nb % 4 == 0 ? 4 : g.Nb % 2 == 0 ? 2 : g.Nb >= 512 ? VEC : 1;
+}
 
 // Lanes on a row, as a power of two
 int lane_shift(const CubeGeom &g)
@@ -121,16 +157,16 @@ int epilogue_bwd(const CubeGeom &g, int kind, int z_dtype, int dy_dtype, int dz_
         typedef decltype(td) TD;
         constexpr int KIND = decltype(kind_c)::value;
         float *part = dbias_diag ? workspace : nullptr;
-        auto of_width = [&](auto v) {
-            hipLaunchKernelGGL((epilogue_bwd_kernel<KIND, TZ, TG, TD, decltype(v)::value>), grid, dim3(256), 0, stream, g, RG, NRG, shift,
-                               static_cast<const TZ *>(z), static_cast<const TG *>(dy), static_cast<TD *>(dz), part);
+        auto of_width = [&](auto v, auto loose) {
+            hipLaunchKernelGGL((epilogue_bwd_kernel<KIND, TZ, TG, TD, decltype(v)::value, decltype(loose)::value>), grid, dim3(256), 0, stream, g,
+                               RG, NRG, shift, static_cast<const TZ *>(z), static_cast<const TG *>(dy), static_cast<TD *>(dz), part);
         };
-        switch (V) {
-        case VEC: of_width(std::integral_constant<int, VEC>{}); break;
-        case 4: of_width(std::integral_constant<int, 4>{}); break;
-        case 2: of_width(std::integral_constant<int, 2>{}); break;
-        default: of_width(std::integral_constant<int, 1>{});
-        }
+        const std::integral_constant<int, VEC> eight{};
+        if (g.Nb % V) of_width(eight, std::true_type{});
+        else if (V == VEC) of_width(eight, std::false_type{});
+        else if (V == 4) of_width(std::integral_constant<int, 4>{}, std::false_type{});
+        else if (V == 2) of_width(std::integral_constant<int, 2>{}, std::false_type{});
+        else of_width(std::integral_constant<int, 1>{}, std::false_type{});
         return launch_status();
     };
     const float f = 0.f;

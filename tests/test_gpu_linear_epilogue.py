@@ -356,3 +356,10 @@ def test_fp8_operands_with_fp32_results(q, axis, M, K, N, shard, z):
             np.testing.assert_array_equal(zt, layer.z0)
         ref = np.maximum(layer.z0, 0.0) + (0.0 if res is None else res)
         np.testing.assert_array_equal(y, rounded(ref, shard))
+
+
+@pytest.mark.parametrize("q,axis,M,N", [(1, "y", 700, 4101), (1, "z", 900, 513), (3, "y", 99, 4599), (1, "y", 3, 2055), (1, "z", 600, 1026), (2, "y", 400, 2052), (1, "y", 5000, 511)])
+@pytest.mark.parametrize("zt,gt,dt", [("bf16", "bf16", "bf16"), ("f32", "bf16", "f32"), ("bf16", "f32", "bf16")])
+def test_epilogue_bwd_odd_blocks(q, axis, M, N, zt, gt, dt):
+    epilogue_bwd(q, axis, M, N, "relu", zt, gt, dt, in_place=gt == dt)
+    epilogue_bwd(q, axis, M, N, "gelu", zt, gt, dt, "normal", with_db=False)
