@@ -84,6 +84,13 @@ template <int KIND> __device__ __forceinline__ float act_slope(float z)
     return f.cdf + z * f.pdf;
 }
 
+// The activation of a product's epilogue: the rectifier keeps NaN.  (The passes over stored activations make it 0, as they always have.)
+template <int KIND> __device__ __forceinline__ float epilogue_act(float z)
+{
+    if (KIND == CUBE3D_ACT_RELU) return z <= 0.f ? 0.f : z;
+    return act_value<KIND>(z);
+}
+
 // A product's epilogue on one value z of the fp32 result, which sits at element `at` of the output (and of residual and Z): keeps
 // Z and returns y = act(z) + residual.
 __device__ __forceinline__ float epilogue_element(const Epilogue &e, float z, int64_t at)
@@ -92,7 +99,7 @@ __device__ __forceinline__ float epilogue_element(const Epilogue &e, float z, in
         if (e.z_f32) static_cast<float *>(e.z)[at] = z;
         else static_cast<unsigned short *>(e.z)[at] = f32_to_bf16_bits(z);
     }
-    float y = e.act == CUBE3D_ACT_GELU ? act_value<CUBE3D_ACT_GELU>(z) : e.act == CUBE3D_ACT_RELU ? act_value<CUBE3D_ACT_RELU>(z) : z;
+    float y = e.act == CUBE3D_ACT_GELU ? epilogue_act<CUBE3D_ACT_GELU>(z) : e.act == CUBE3D_ACT_RELU ? epilogue_act<CUBE3D_ACT_RELU>(z) : z;
     if (e.residual)
         y += e.residual_f32 ? static_cast<const float *>(e.residual)[at] : bf16_bits_to_f32(static_cast<const unsigned short *>(e.residual)[at]);
     return y;

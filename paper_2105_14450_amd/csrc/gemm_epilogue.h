@@ -42,14 +42,14 @@ template <int N> __device__ __forceinline__ void activate(int act, bool exact, f
     if (act == CUBE3D_ACT_GELU) {
         if (exact) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = act_value<CUBE3D_ACT_GELU>(x[e]);
+            for (int e = 0; e < N; ++e) x[e] = epilogue_act<CUBE3D_ACT_GELU>(x[e]);
         } else {
 #pragma unroll
             for (int e = 0; e < N; ++e) x[e] = gelu_short(x[e]);
         }
     } else if (act == CUBE3D_ACT_RELU) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = act_value<CUBE3D_ACT_RELU>(x[e]);
+        for (int e = 0; e < N; ++e) x[e] = epilogue_act<CUBE3D_ACT_RELU>(x[e]);
     }
 }
 
