@@ -422,7 +422,8 @@ int cube3d_activation_bwd(int kind, int z_dtype, int dh_dtype, int dz_dtype, int
  *     Z = X W + b,   Y = act(Z) + R,
  * with the sum, the bias, the activation (of the fp32 value, before Z is rounded) and the residual in fp32 and one
  * rounding each of Y (to shard_dtype) and Z (to z_dtype).  All of X, W, Y, b as for virtual_cube_linear_fwd.
- *   activation   a cube3d_activation; CUBE3D_ACT_NONE: Y = Z + R.  NaN stays NaN (cube3d_activation_fwd's rectifier makes it 0)
+ *   activation   a cube3d_activation; CUBE3D_ACT_NONE: Y = Z + R.  NaN stays NaN (cube3d_activation_fwd's rectifier makes it 0);
+ *                GELU of -infinity is NaN (as there)
  *   bias_diag    NULL, or the diagonal storage of b (fp32)
  *   residual     NULL, or R as a cube of Y shards of residual_dtype (F32 or BF16).  May be Y itself if the two
  *                types agree: the sum is then formed in place

@@ -21,11 +21,11 @@ __device__ __forceinline__ bf16x8 widen_fp8(i32x2 codes)
 // GELU where nothing hides its arithmetic: z Phi(z) = max(z, 0) - t Phi(-t) with t = |z|, and Phi(-t) = 2^(-p(t)), p(t) = 1 + t
 // times a degree-6 polynomial (equal-ripple fit of -log2 Phi(-t) on [0, 6]; beyond, p keeps growing: 30 at 6).  15 issue slots an
 // element (v_exp_f32 counts four) for the 25 of act_value, which is closer: t Phi(-t) is within 7e-7 here and Phi(-t) within
-// 6e-6 of itself, a thousandth of a bf16 rounding; fp32 results take act_value.  (t is cut at 64, where Phi(-t) is zero, for the sake
-// of infinities; NaN passes the comparison by.)
+// 6e-6 of itself, a thousandth of a bf16 rounding; fp32 results take act_value.  (t is cut at 64 on the upper side,
+// where Phi(-t) is zero, so that +infinity stays itself; -infinity gives NaN, as z Phi(z) does everywhere else, and NaN passes the comparison by.)
 __device__ __forceinline__ float gelu_short(float z)
 {
-    const float a = fabsf(z), t = a > 64.f ? 64.f : a;
+    const float t = z > 64.f ? 64.f : fabsf(z);
     float s = 1.793782303e-06f;
     s = fmaf(s, t, -6.072620090e-05f);
     s = fmaf(s, t, 9.231860749e-04f);

@@ -74,3 +74,34 @@ def test_rectifier_keeps_nan(M, K, N, dtype):
 @pytest.mark.parametrize("M,K,N", [(4, 2048, 256), (64, 4096, 520), (256, 512, 512), (1004, 1028, 1004), (130, 333, 77), (3001, 17, 1031)])
 def test_rectifier_keeps_nan_in_fp32(M, K, N):
     check_relu(M, K, N, "f32", [p for p in PARTS if p[2] == "f32"] + PARTS[:1])
+
+
+def check_gelu(M, K, N, dtype, parts):
+    """Against z Phi(z) as it stands: +infinity stays, -infinity times zero is NaN, and NaN stays.  Finite ones: a bf16 rounding (2^-8) and
+    1e-6, or 1e-6 and 4e-6 of the value in fp32 (the evaluation's own error; |z| is 1e4 at most, the sum exact)."""
+    X, W, R, b = operands(M, K, N, dtype)
+    ref = X.double() @ W.double() + b.double()
+    if dtype != "fp8_e4m3":
+        assert set(ref[ROW_INF].tolist()) == {float("inf"), -float("inf")}
+    for residual, z, out in parts:
+        Y, Z = run(M, K, N, dtype, "gelu", residual, z, out, X, W, R, b)
+        if z:
+            same(Z, ref)
+        want = ref * torch.special.ndtr(ref) + (R.double() if residual else 0.0)
+        if dtype != "fp8_e4m3":
+            assert bool((want[ROW_INF].isnan() == (ref[ROW_INF] < 0)).all())
+        fine = want.isfinite()
+        assert torch.equal(Y.isnan(), want.isnan()) and torch.equal(Y[~fine & ~want.isnan()], want[~fine & ~want.isnan()].to(Y.dtype))
+        size = want[fine].abs() + (R.double().abs()[fine] if residual else 0.0)
+        assert bool(((Y[fine].double() - want[fine]).abs() <= (1.01 * 2.0 ** -8 if out == "bf16" else 4e-6) * size + 1e-6).all())
+
+
+@pytest.mark.parametrize("M,K,N", SIZES)
+@pytest.mark.parametrize("dtype", ["bf16", "fp8_e4m3"])
+def test_gelu_of_infinities_is_the_same_everywhere(M, K, N, dtype):
+    check_gelu(M, K, N, dtype, PARTS)
+
+
+@pytest.mark.parametrize("M,K,N", [(4, 2048, 256), (64, 4096, 520), (256, 512, 512), (1004, 1028, 1004), (130, 333, 77), (3001, 17, 1031)])
+def test_gelu_of_infinities_in_fp32(M, K, N):
+    check_gelu(M, K, N, "f32", [p for p in PARTS if p[2] == "f32"] + PARTS[:1])
