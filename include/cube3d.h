@@ -533,7 +533,7 @@ int virtual_cube_norm_bwd(const cube3d_matrix *m, const cube3d_norm *norm, const
  *       aligned, else CUBE3D_EWORKSPACE.
  *   cube3d_grad_clip:  out = f * g  with  f = scale * min(1, max_norm / (scale * sqrt(*sumsq)))
  *       rounded once to the type of out[k], an array of as many elements as grads[k].  f is formed on the device, in 64
- *       bits, and rounded to fp32.  A norm that is not finite leaves f = scale: the caller sees it in *norm.
+ *       bits, and rounded to fp32.  A norm that is not finite in fp32 leaves f = scale: the caller sees it in *norm.
  *       out[k] may be grads[k] itself (same address and type; nothing is written where f is 1).  Any other overlap
  *       among the arrays of `out` or of them with those of `grads` is refused (CUBE3D_EINVAL).
  * scale: positive and finite (the reciprocal of a loss scale, or of a number of accumulated batches); max_norm: positive.

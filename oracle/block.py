@@ -143,4 +143,6 @@ def gradient_norm(grads):
 
 def clip_factor(norm, max_norm, scale=1.0):
     norm = scale * norm
-    return scale * min(1.0, max_norm / norm) if np.isfinite(norm) and norm > 0 else scale
+    with np.errstate(over="ignore"):
+        finite = np.isfinite(np.float32(norm))      # (as the norm is stored)
+    return scale * min(1.0, max_norm / norm) if finite and norm > 0 else scale

@@ -134,8 +134,9 @@ __device__ __forceinline__ void scale_unit(const void *from, void *to, int64_t n
 __global__ __launch_bounds__(LANES) void grad_clip_kernel(const Arrays a, double scale, double max_norm, const double *__restrict__ sumsq)
 {
     // (the same few operations in every lane, so that no launch is needed for one number)
+    // A norm is finite where grad_norm_finish_kernel's fp32 value is: the caller sees there what is done here.
     const double norm = scale * sqrt(*sumsq);
-    const float f = (float)(norm > max_norm && norm < __builtin_huge_val() ? scale * (max_norm / norm) : scale);
+    const float f = (float)(norm > max_norm && (float)norm < __builtin_huge_valf() ? scale * (max_norm / norm) : scale);
     for (int64_t u = blockIdx.x; u < a.first[a.count]; u += gridDim.x) {
         const int t = array_of(a, u);
         if (f == 1.f && a.src[t] == a.dst[t]) continue;
