@@ -220,13 +220,13 @@ __global__ __launch_bounds__(LANES) void norm_bwd_rows_kernel(const NormArgs a, 
 }
 
 // Everything that remains is element-wise but for the column sums: a workgroup takes 64 V columns of a group of rows, a lane V of
-// every fourth row, and leaves partial sums [group][vector][column].
+// every fourth row, and leaves partial sums [group][vector][column].  first_tile: of this launch (launch_in_parts).
 template <typename TS, typename TB, int V>
 __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a, const float *__restrict__ scalars, float *__restrict__ partials,
-                                                               int rows_per_group, int wanted)
+                                                               int rows_per_group, int wanted, int first_tile)
 {
     __shared__ float lds[4][64 * V];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = (blockIdx.x * 64 + lane) * V;
+    const int tile = first_tile + blockIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = (tile * 64 + lane) * V;
     const bool live = c < a.cols;
     const int64_t col = axis_offset_fast(a.col, live ? c : 0);
     ColumnParams<V> p;
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a,
         for (int e = 0; e < V; ++e) lds[wave][e * 64 + lane] = sum[v][e];
         __syncthreads();
         for (int x = threadIdx.x; x < 64 * V; x += 256) {
-            const int at = x % V * 64 + x / V, column = blockIdx.x * 64 * V + x;
+            const int at = x % V * 64 + x / V, column = tile * 64 * V + x;
             if (column < a.cols)
                 partials[((int64_t)blockIdx.y * VECTORS + v) * a.cols + column] = ((lds[0][at] + lds[1][at]) + lds[2][at]) + lds[3][at];
         }
@@ -301,10 +301,10 @@ __global__ __launch_bounds__(256) void norm_bwd_columns_kernel(const NormArgs a,
 }
 
 // The groups' partial sums of one vector, in ascending order, to its diagonal storage (zeros off the diagonal).  A workgroup takes
-// 64 of the Cs columns of a processor, its wavefronts runs of the groups.
+// 64 of the Cs columns of a processor, its wavefronts runs of the groups.  first_tile: of this launch.
 constexpr int FINISH_WAVES = 16;
 __global__ __launch_bounds__(64 * FINISH_WAVES) void norm_bwd_finish_kernel(const NormArgs a, const float *__restrict__ partials, int groups,
-                                                                            cube3d_norm_params out)
+                                                                            cube3d_norm_params out, int first_tile)
 {
     __shared__ float lds[FINISH_WAVES][64];
     float *const vectors[VECTORS] = {out.post_gamma, out.post_beta, out.gate, out.pre_gamma, out.pre_beta};
@@ -313,7 +313,7 @@ __global__ __launch_bounds__(64 * FINISH_WAVES) void norm_bwd_finish_kernel(cons
     for (int v = 1; v < VECTORS; ++v)
         if ((int)blockIdx.z == v) dst = vectors[v];
     if (!dst) return;
-    const int q = a.q, Cs = a.vec.P2, lane = threadIdx.x % 64, wave = threadIdx.x / 64, x = blockIdx.x * 64 + lane;
+    const int q = a.q, Cs = a.vec.P2, lane = threadIdx.x % 64, wave = threadIdx.x / 64, x = (first_tile + blockIdx.x) * 64 + lane;
     const int proc = blockIdx.y, l = proc % q, j = proc / q % q, i = proc / (q * q);
     const bool live = x < Cs;
     if (j != l) {
@@ -1022,12 +1022,24 @@ size_t norm_bwd_workspace(const NormArgs &a)
 
 namespace {
 
+// A launch has fewer than 2^32 work-items along a grid dimension: `tiles` workgroups of `lanes` in as many launches as that takes.
+template <typename F> int launch_in_parts(int64_t tiles, int lanes, F &&f)
+{
+    const int64_t most = (1ll << 32) / lanes - 1;
+    for (int64_t first = 0; first < tiles; first += most) {
+        f((unsigned)(tiles - first < most ? tiles - first : most), (int)first);
+        if (const int rc = launch_status(); rc != CUBE3D_OK) return rc;
+    }
+    return CUBE3D_OK;
+}
+
 int finish(const NormArgs &a, const float *partials, unsigned groups, const cube3d_norm_params &gradients, hipStream_t stream)
 {
     const unsigned q3 = (unsigned)(a.q * a.q * a.q);
-    hipLaunchKernelGGL(norm_bwd_finish_kernel, dim3((unsigned)((a.vec.P2 + 63) / 64), q3, VECTORS), dim3(64 * FINISH_WAVES), 0, stream, a,
-                       partials, (int)groups, gradients);
-    return launch_status();
+    return launch_in_parts(((int64_t)a.vec.P2 + 63) / 64, 64 * FINISH_WAVES, [&](unsigned tiles, int first) {
+        hipLaunchKernelGGL(norm_bwd_finish_kernel, dim3(tiles, q3, VECTORS), dim3(64 * FINISH_WAVES), 0, stream, a, partials, (int)groups, gradients,
+                           first);
+    });
 }
 
 }  // namespace
@@ -1101,9 +1113,10 @@ int norm_bwd(const NormArgs &a, const cube3d_norm_params &gradients, void *works
                     hipLaunchKernelGGL((norm_bwd_rows_kernel<TS, TB, V, LANES>), wide, dim3(LANES), 0, stream, a, scalars);
                 });
             if (const int e = launch_status(); e != CUBE3D_OK) return e;
-            hipLaunchKernelGGL((norm_bwd_columns_kernel<TS, TB, V>), dim3((unsigned)((a.cols + 64 * V - 1) / (64 * V)), groups), dim3(256), 0,
-                               stream, a, scalars, partials, per, wanted);
-            return launch_status();
+            return launch_in_parts(((int64_t)a.cols + 64 * V - 1) / (64 * V), 256, [&](unsigned tiles, int first) {
+                hipLaunchKernelGGL((norm_bwd_columns_kernel<TS, TB, V>), dim3(tiles, groups), dim3(256), 0, stream, a, scalars, partials, per, wanted,
+                                   first);
+            });
         });
     });
     return rc != CUBE3D_OK || !a.sums ? rc : finish(a, partials, groups, gradients, stream);
