@@ -181,11 +181,12 @@ int launch_layout(const GemmArgs &g)
                                g.Mo, g.No, g.Kc, g.lda, g.ldb, g.ldc, g.strideA, g.strideB, g.strideC, g.alpha, maps, epi);
             return launch_status();
         };
-        if constexpr (sizeof(TIn) == 1) {
-            if (widens(g)) return launch(std::true_type{});
-            if (sizeof(TOut) == 4) return CUBE3D_EINVAL;        // (widened always)
+        if constexpr (sizeof(TIn) == 1 && sizeof(TOut) == 4) return launch(std::true_type{});      // (widens)
+        else {
+            if constexpr (sizeof(TIn) == 1)
+                if (widens(g)) return launch(std::true_type{});
+            return launch(std::false_type{});
         }
-        return launch(std::false_type{});
     }
 #define CUBE3D_LAUNCH(AKV, BKV, MP)                                                                               \
     hipLaunchKernelGGL((gemm_generic_kernel<TIn, TOut, AKV, BKV, MP>), grid, block, 0, g.stream, A, B, C, g.Mo, \
