@@ -20,9 +20,10 @@ __device__ __forceinline__ bf16x8 widen_fp8(i32x2 codes)
 
 // GELU where nothing hides its arithmetic: z Phi(z) = max(z, 0) - t Phi(-t) with t = |z|, and Phi(-t) = 2^(-p(t)), p(t) = 1 + t
 // times a degree-6 polynomial (equal-ripple fit of -log2 Phi(-t) on [0, 6]; beyond, p keeps growing: 30 at 6).  15 issue slots an
-// element (v_exp_f32 counts four) for the 25 of act_value, which is closer: t Phi(-t) is within 7e-7 here and Phi(-t) within
-// 6e-6 of itself, a thousandth of a bf16 rounding; fp32 results take act_value.  (t is cut at 64 on the upper side,
-// where Phi(-t) is zero, so that +infinity stays itself; -infinity gives NaN, as z Phi(z) does everywhere else, and NaN passes the comparison by.)
+// element (v_exp_f32 counts four) for the 25 of act_value, which fp32 results take.  t Phi(-t) is within 7e-7 here; up to t = 6 Phi(-t) is
+// within 8e-6 of itself, a 240th of half a bf16 step (2^-9 of a value at least); beyond, where t Phi(-t) is below 6e-9, it is within 5e-14
+// (of itself 3e-4 at 7, and from 8 on more than half a step).  t is cut at 64 on the upper side, where Phi(-t) is zero, so that
+// +infinity stays itself; -infinity gives NaN, as z Phi(z) does everywhere else, and NaN passes the comparison by.
 __device__ __forceinline__ float gelu_short(float z)
 {
     const float t = z > 64.f ? 64.f : fabsf(z);
