@@ -434,6 +434,8 @@ int cube3d_activation_bwd(int kind, int z_dtype, int dh_dtype, int dz_dtype, int
  * contraction and joined in `workspace`: device scratch, 16-byte aligned, of at least
  * cube3d_epilogue_workspace_bytes(desc, CUBE3D_OP_FWD) bytes (may be NULL when that is 0, else CUBE3D_EWORKSPACE);
  * contents undefined afterwards.  The order of an element's sum is fixed by the shape: two calls give the same bits.
+ * What the calls here and below write (results, workspaces) may overlap nothing else of the call but where it says so:
+ * CUBE3D_EINVAL.
  *
  * virtual_cube_linear_epilogue_bwd: the backward pass of the epilogue,
  *     dZ = dY * act'(Z),   db = column sums of dZ   (Algorithm 8, as in virtual_cube_bias_bwd),
@@ -535,7 +537,7 @@ int virtual_cube_norm_bwd(const cube3d_matrix *m, const cube3d_norm *norm, const
  *       rounded once to the type of out[k], an array of as many elements as grads[k].  f is formed on the device, in 64
  *       bits, and rounded to fp32.  A norm that is not finite in fp32 leaves f = scale: the caller sees it in *norm.
  *       out[k] may be grads[k] itself (same address and type; nothing is written where f is 1).  Any other overlap
- *       among the arrays of `out` or of them with those of `grads` is refused (CUBE3D_EINVAL).
+ *       among the arrays of `out` or of them with those of `grads` or with *sumsq is refused (CUBE3D_EINVAL).
  * scale: positive and finite (the reciprocal of a loss scale, or of a number of accumulated batches); max_norm: positive.
  */
 typedef struct cube3d_tensor {

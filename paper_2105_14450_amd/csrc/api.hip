@@ -1,5 +1,6 @@
 // C-ABI entry points: argument validation on the host, then dispatch to the
 // kernels.  Nothing here touches the device before every check has passed.
+#include <initializer_list>
 #include <mutex>
 
 #include "common.h"
@@ -104,6 +105,36 @@ size_t workspace_for(const GemmArgs &a)
     return gemm_fast_workspace(a, gemm_fast_plan(a));
 }
 
+// An array of a call (nullptr: absent).  What a call writes may share memory with nothing else, but for what it allows in place.
+struct Span {
+    const void *p;
+    int64_t elements;
+    int size;
+};
+
+Span span(const void *p, int64_t rows, int64_t cols, int size)
+{
+    int64_t n;
+    return Span{p, __builtin_mul_overflow(rows, cols, &n) ? INT64_MAX : n, size};
+}
+
+bool overlap(const Span &a, const Span &b)
+{
+    if (!a.p || !b.p) return false;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return x <= y ? (int64_t)((y - x) / a.size) < a.elements : (int64_t)((x - y) / b.size) < b.elements;
+}
+
+bool overlaps_any(const Span &a, std::initializer_list<Span> others)
+{
+    for (const Span &b : others)
+        if (overlap(a, b)) return true;
+    return false;
+}
+
+// (in place: the same address and type)
+bool overlaps_but_in_place(const Span &a, const Span &b) { return overlap(a, b) && !(a.p == b.p && a.size == b.size); }
+
 // The first kernel family that takes the product: tile-aligned sizes, then any size, then element by element.
 int run_gemm(const GemmArgs &a)
 {
@@ -111,6 +142,13 @@ int run_gemm(const GemmArgs &a)
         if (const int splits = gemm_rows_plan(a); splits > 0) {
             const size_t need = gemm_rows_workspace(a, splits);
             if (need > 0 && (!a.workspace || a.workspace_bytes < need)) return CUBE3D_EWORKSPACE;
+            const int in = elem_size(a.in_dtype), out = elem_size(a.out_dtype);
+            const Epilogue &e = *a.epilogue;
+            if (need > 0 && overlaps_any(Span{a.workspace, (int64_t)need, 1},
+                                         {Span{a.A, a.Mo * a.Kc, in}, Span{a.B, a.Kc * a.No, in}, Span{a.C, a.Mo * a.No, out},
+                                          Span{a.maps->bias, axis_offset(a.maps->bias_n, a.No - 1) + 1, 4},
+                                          Span{e.residual, a.Mo * a.No, e.residual_f32 ? 4 : 2}, Span{e.z, a.Mo * a.No, e.z_f32 ? 4 : 2}}))
+                return CUBE3D_EINVAL;
             return gemm_rows(a, splits);
         }
         if (widens(a)) {        // (not by the tuned kernel, which has the fp8 instructions only)
@@ -663,6 +701,14 @@ cube3d_norm_params used_params(const cube3d_norm &norm, cube3d_norm_params p, bo
     return p;
 }
 
+// Whether `a` overlaps any of the vectors of `p`
+bool overlaps_any(const Span &a, const cube3d_norm_params &p, const NormArgs &norm)
+{
+    for (const float *v : {p.post_gamma, p.post_beta, p.gate, p.pre_gamma, p.pre_beta})
+        if (overlap(a, Span{v, (int64_t)norm.q * norm.cols, 4})) return true;
+    return false;
+}
+
 int check_tensors(const cube3d_tensor *t, int count)
 {
     if (count < 0 || (count > 0 && !t)) return CUBE3D_EINVAL;
@@ -726,20 +772,20 @@ int virtual_cube_linear_fwd_fused(const cube3d_desc *desc, const cube3d_epilogue
     if (epilogue->residual && !f32_or_bf16(epilogue->residual_dtype)) return CUBE3D_EDTYPE;
     if (epilogue->z && !f32_or_bf16(epilogue->z_dtype)) return CUBE3D_EDTYPE;
     if (misaligned(epilogue->residual) || misaligned(epilogue->z) || misaligned(workspace)) return CUBE3D_EINVAL;
-    // in place only element by element: Z may not be Y, nor either of them a residual of another type
-    if (epilogue->z && (epilogue->z == Y_shards || epilogue->z == epilogue->residual)) return CUBE3D_EINVAL;
-    if (epilogue->residual == Y_shards && Y_shards && epilogue->residual_dtype != desc->shard_dtype) return CUBE3D_EINVAL;
     const Epilogue e{epilogue->activation, epilogue->residual && epilogue->residual_dtype == CUBE3D_F32,
                      epilogue->z && epilogue->z_dtype == CUBE3D_F32, epilogue->residual, epilogue->z};
     if (!X_shards || !W_shards || !Y_shards || misaligned(X_shards) || misaligned(W_shards) || misaligned(Y_shards) ||
         misaligned(epilogue->bias_diag))
         return CUBE3D_EINVAL;
-    for (const void *operand : {X_shards, W_shards})
-        if (operand == Y_shards || operand == epilogue->z) return CUBE3D_EINVAL;
     GemmMaps maps;
     GemmArgs a;
     rc = build_cube_product(desc, CUBE3D_OP_FWD, X_shards, W_shards, epilogue->bias_diag, Y_shards, stream, &maps, &a);
     if (rc != CUBE3D_OK) return rc;
+    const int in = elem_size(desc->in_dtype);
+    const Span x{X_shards, a.Mo * a.Kc, in}, w{W_shards, a.Kc * a.No, in}, bias{epilogue->bias_diag, desc->q * a.No, 4};
+    const Span r{epilogue->residual, a.Mo * a.No, e.residual_f32 ? 4 : 2}, z{epilogue->z, a.Mo * a.No, e.z_f32 ? 4 : 2};
+    const Span y{Y_shards, a.Mo * a.No, elem_size(a.out_dtype)};
+    if (overlaps_any(y, {x, w, bias, z}) || overlaps_any(z, {x, w, bias, r}) || overlaps_but_in_place(y, r)) return CUBE3D_EINVAL;
     a.epilogue = &e;
     a.workspace = workspace;
     a.workspace_bytes = workspace_bytes;
@@ -758,8 +804,11 @@ int virtual_cube_linear_epilogue_bwd(const cube3d_desc *desc, int kind, int z_dt
     if (!Z_shards || !dY_shards || !dZ_shards) return CUBE3D_EINVAL;
     if (misaligned(Z_shards) || misaligned(dY_shards) || misaligned(dZ_shards) || misaligned(dbias_diag) || misaligned(workspace))
         return CUBE3D_EINVAL;
-    if (dZ_shards == Z_shards || (dZ_shards == dY_shards && dz_dtype != dy_dtype)) return CUBE3D_EINVAL;
-    if (dbias_diag && (!workspace || workspace_bytes < epilogue_bwd_workspace(g))) return CUBE3D_EWORKSPACE;
+    const size_t need = dbias_diag ? epilogue_bwd_workspace(g) : 0;
+    if (dbias_diag && (!workspace || workspace_bytes < need)) return CUBE3D_EWORKSPACE;
+    const Span z = span(Z_shards, g.M, g.N, elem_size(z_dtype)), dy = span(dY_shards, g.M, g.N, elem_size(dy_dtype));
+    const Span dz = span(dZ_shards, g.M, g.N, elem_size(dz_dtype)), db = span(dbias_diag, g.q, g.N, 4), ws{workspace, (int64_t)need, 1};
+    if (overlap(dz, z) || overlaps_but_in_place(dz, dy) || overlap(db, dz) || overlaps_any(ws, {z, dy, dz, db})) return CUBE3D_EINVAL;
     return epilogue_bwd(g, kind, z_dtype, dy_dtype, dz_dtype, Z_shards, dY_shards, dZ_shards, static_cast<float *>(dbias_diag),
                         static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
 }
@@ -782,9 +831,14 @@ int virtual_cube_norm_fwd(const cube3d_matrix *m, const cube3d_norm *norm, const
     if (!u && norm->post_kind != CUBE3D_NORM_NONE) return CUBE3D_EINVAL;
     for (const void *p : {x, u, (const void *)r, (const void *)n, (const void *)stats})
         if (misaligned(p)) return CUBE3D_EINVAL;
-    if (n && (n == x || n == u || n == r)) return CUBE3D_EINVAL;      // n is written while x and u are still read
-    if (r && r == u) return CUBE3D_EINVAL;
+    const int64_t all = a.rows * a.cols;
+    const int se = a.stream_f32 ? 4 : 2, be = a.block_f32 ? 4 : 2;
+    const Span xs{x, all, se}, us{u, all, be}, rs{r, all, se}, ns{n, all, be}, st{stats, 4 * a.rows, 4};
+    // (n is written while x and u are still read)
+    if (overlaps_any(ns, {xs, us, rs}) || overlap(rs, us) || overlaps_but_in_place(rs, xs) || overlaps_any(st, {xs, us, rs, ns})) return CUBE3D_EINVAL;
     a.p = used_params(*norm, *params, u != nullptr);
+    for (const Span &result : {rs, ns, st})
+        if (overlaps_any(result, a.p, a)) return CUBE3D_EINVAL;
     a.x = x; a.u = u;
     a.r_out = r; a.n_out = n; a.stats_out = stats;
     return norm_fwd(a, static_cast<hipStream_t>(stream));
@@ -810,15 +864,22 @@ int virtual_cube_norm_bwd(const cube3d_matrix *m, const cube3d_norm *norm, const
     if (!dx && !du && !sums) return CUBE3D_EINVAL;
     for (const void *p : {(const void *)stats, dr, dn, r, u, (const void *)dx, (const void *)du, (const void *)workspace})
         if (misaligned(p)) return CUBE3D_EINVAL;
-    for (const void *in : {dn, r, u})
-        if (in && (in == dx || in == du)) return CUBE3D_EINVAL;
-    if (du && (du == dr || du == dx)) return CUBE3D_EINVAL;
+    const int64_t all = a.rows * a.cols;
+    const int se = a.stream_f32 ? 4 : 2, be = a.block_f32 ? 4 : 2;
+    const Span drs{dr, all, se}, dns{dn, all, be}, rs{r, all, se}, us{u, all, be}, st{stats, 4 * a.rows, 4}, dxs{dx, all, se}, dus{du, all, be};
+    if (overlaps_any(dxs, {dns, rs, us, st}) || overlaps_but_in_place(dxs, drs) || overlaps_any(dus, {drs, dns, rs, us, st, dxs})) return CUBE3D_EINVAL;
+    a.p = used_params(*norm, *params, u != nullptr);
+    for (const Span &result : {dxs, dus})
+        if (overlaps_any(result, a.p, a) || overlaps_any(result, d, a)) return CUBE3D_EINVAL;
+    // (the gradients of vectors are written behind everything that is read but the workspace)
     const float *vectors[] = {d.post_gamma, d.post_beta, d.gate, d.pre_gamma, d.pre_beta};
     for (int i = 0; i < 5; ++i)
         for (int k = 0; k < i; ++k)
-            if (vectors[i] && vectors[i] == vectors[k]) return CUBE3D_EINVAL;
-    if (!workspace || workspace_bytes < norm_bwd_workspace(a)) return CUBE3D_EWORKSPACE;
-    a.p = used_params(*norm, *params, u != nullptr);
+            if (overlap(Span{vectors[i], (int64_t)a.q * a.cols, 4}, Span{vectors[k], (int64_t)a.q * a.cols, 4})) return CUBE3D_EINVAL;
+    const size_t need = norm_bwd_workspace(a);
+    if (!workspace || workspace_bytes < need) return CUBE3D_EWORKSPACE;
+    const Span ws{workspace, (int64_t)need, 1};
+    if (overlaps_any(ws, {drs, dns, rs, us, st, dxs, dus}) || overlaps_any(ws, a.p, a) || overlaps_any(ws, d, a)) return CUBE3D_EINVAL;
     a.x = r; a.u = u;
     a.stats = stats; a.dr = dr; a.dn = dn; a.dx = dx; a.du = du;
     a.read_u = post || d.gate;
@@ -841,6 +902,9 @@ int cube3d_grad_norm(const cube3d_tensor *grads, int count, float scale, double 
         return CUBE3D_EINVAL;
     const size_t need = (size_t)grad_norm_partials(grads, count) * sizeof(double);
     if (need > 0 && (!workspace || workspace_bytes < need)) return CUBE3D_EWORKSPACE;
+    if (overlap(Span{sumsq, 1, 8}, Span{norm, 1, 4})) return CUBE3D_EINVAL;
+    for (int k = 0; k < count; ++k)
+        if (overlap(Span{workspace, (int64_t)need, 1}, Span{grads[k].data, grads[k].n, elem_size(grads[k].dtype)})) return CUBE3D_EINVAL;
     return grad_norm(grads, count, scale, sumsq, norm, static_cast<double *>(workspace), static_cast<hipStream_t>(stream));
 }
 
@@ -852,8 +916,10 @@ int cube3d_grad_clip(const cube3d_tensor *grads, const cube3d_tensor *out, int c
     if (rc != CUBE3D_OK) return rc;
     if (!(scale > 0.f) || scale > 3.4028235e38f || !(max_norm > 0.f)) return CUBE3D_EINVAL;
     if (!sumsq || reinterpret_cast<uintptr_t>(sumsq) % 8) return CUBE3D_EINVAL;
-    for (int k = 0; k < count; ++k)
+    for (int k = 0; k < count; ++k) {
         if (grads[k].n != out[k].n) return CUBE3D_ESHAPE;
+        if (overlap(Span{sumsq, 1, 8}, Span{out[k].data, out[k].n, elem_size(out[k].dtype)})) return CUBE3D_EINVAL;
+    }
     rc = check_clip_overlap(grads, out, count);
     if (rc != CUBE3D_OK) return rc;
     return grad_clip(grads, out, count, scale, max_norm, sumsq, static_cast<hipStream_t>(stream));
