@@ -238,7 +238,7 @@ struct NormArgs {
     bool read_u, sums;              // u is read; any column sum is wanted
 };
 int norm_fwd(const NormArgs &a, hipStream_t stream);
-size_t norm_bwd_workspace(const NormArgs &a);      // of rows, cols alone
+size_t norm_bwd_workspace(const NormArgs &a);      // of sizes, placement, kinds, the stream's type and the number of CUs
 int norm_bwd(const NormArgs &a, const cube3d_norm_params &gradients, void *workspace, hipStream_t stream);
 
 // Gradient norm and clipping over lists of arrays that the caller has checked.  Partial sums (doubles) of grad_norm:

@@ -85,7 +85,8 @@ struct Fp8Rows {
     }
 };
 
-// fp32 results: the operands widened to bf16, whose instruction has the same layout (see widens)
+// fp32 results: the operands widened to bf16, whose instruction has the same layout (see widens).  bf16 results do without: us not widened /
+// widened, 16 x 16384 x 4096 18.1 / 18.6, 1 x 8192 x 8192 17.8 / 18.7, 64 x 8192 x 8192 25.9 / 27.7.
 struct Fp8WideRows : Fp8Rows {
     __device__ static __forceinline__ f32x4 mfma(Frag a, Frag b, f32x4 c)
     {

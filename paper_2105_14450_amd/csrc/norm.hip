@@ -752,8 +752,8 @@ template <typename F> int by_width(const NormArgs &a, F &&f)
 }
 
 // Rows of up to 16384 columns, sixteen a lane: the registers hold a row and nothing else, so the parameters are read row by row and the
-// column sums lie in LDS, where a lane finds its own (16 columns x 1024 lanes x 4 bytes for each vector asked for).  Where the vectors
-// asked for do not fit, the two passes for any size take the call.  us, here / there: 16384 x 12288 bf16 402 / 668,
+// column sums lie in LDS, where a lane finds its own (16 columns x 4 bytes x the row's lanes for each vector asked for: four vectors up to
+// 9216 columns, three up to 12288, two up to 16384).  Where the vectors asked for do not fit, the two passes for any size take the call.  us, here / there: 16384 x 12288 bf16 402 / 668,
 // 8192 x 16384 271 / 473, 16384 x 12288 with an fp32 stream and both norms 741 / 1300.
 constexpr int LONG_SUMS = 38400;         // floats: 150 KB of the 160
 template <typename TS, typename TB, bool PRE, bool POST>
