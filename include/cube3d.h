@@ -444,7 +444,7 @@ int cube3d_activation_bwd(int kind, int z_dtype, int dh_dtype, int dz_dtype, int
  * the sum of the values before that rounding, in fp32 in a fixed order, in diagonal storage (entries off the
  * diagonal written as zero).  dbias_diag may be NULL: dZ only, no workspace.  Else `workspace` holds at least
  * cube3d_epilogue_workspace_bytes(desc, CUBE3D_OP_BIAS_BWD) bytes.  dZ may be dY itself if the types agree.  The gradient
- * of R is dY; dX and dW follow from dZ by virtual_cube_linear_bwd_dx / _dw.
+ * of R is dY; dX and dW follow from dZ by virtual_cube_linear_bwd_dx / _dw.  M N <= 2^44, else CUBE3D_ESHAPE.
  */
 typedef struct cube3d_epilogue {
     int32_t activation;

@@ -112,12 +112,6 @@ struct Span {
     int size;
 };
 
-Span span(const void *p, int64_t rows, int64_t cols, int size)
-{
-    int64_t n;
-    return Span{p, __builtin_mul_overflow(rows, cols, &n) ? INT64_MAX : n, size};
-}
-
 bool overlap(const Span &a, const Span &b)
 {
     if (!a.p || !b.p) return false;
@@ -654,6 +648,9 @@ bool misaligned(const cube3d_norm_params &p)
     return false;
 }
 
+// Whether a cube of Y shards is one that memory could hold (and the rows of a workgroup of epilogue_bwd an int)
+bool too_large(const CubeGeom &g) { return g.M > (1ll << 44) / g.N; }
+
 // Placement, sizes, types and kinds of a norm call.
 int check_norm(const cube3d_matrix *m, const cube3d_norm *norm, NormArgs *out)
 {
@@ -751,7 +748,7 @@ size_t cube3d_epilogue_workspace_bytes(const cube3d_desc *desc, int op)
 {
     CubeGeom g;
     if (check_desc(desc, &g) != CUBE3D_OK) return 0;
-    if (op == CUBE3D_OP_BIAS_BWD) return epilogue_bwd_workspace(g);
+    if (op == CUBE3D_OP_BIAS_BWD) return too_large(g) ? 0 : epilogue_bwd_workspace(g);
     if (op != CUBE3D_OP_FWD) return 0;
     const Epilogue any{};
     GemmMaps maps;
@@ -799,6 +796,7 @@ int virtual_cube_linear_epilogue_bwd(const cube3d_desc *desc, int kind, int z_dt
     CubeGeom g;
     int rc = check_desc(desc, &g);
     if (rc != CUBE3D_OK) return rc;
+    if (too_large(g)) return CUBE3D_ESHAPE;
     if (kind != CUBE3D_ACT_RELU && kind != CUBE3D_ACT_GELU) return CUBE3D_EINVAL;
     if (!f32_or_bf16(z_dtype) || !f32_or_bf16(dy_dtype) || !f32_or_bf16(dz_dtype)) return CUBE3D_EDTYPE;
     if (!Z_shards || !dY_shards || !dZ_shards) return CUBE3D_EINVAL;
@@ -806,8 +804,8 @@ int virtual_cube_linear_epilogue_bwd(const cube3d_desc *desc, int kind, int z_dt
         return CUBE3D_EINVAL;
     const size_t need = dbias_diag ? epilogue_bwd_workspace(g) : 0;
     if (dbias_diag && (!workspace || workspace_bytes < need)) return CUBE3D_EWORKSPACE;
-    const Span z = span(Z_shards, g.M, g.N, elem_size(z_dtype)), dy = span(dY_shards, g.M, g.N, elem_size(dy_dtype));
-    const Span dz = span(dZ_shards, g.M, g.N, elem_size(dz_dtype)), db = span(dbias_diag, g.q, g.N, 4), ws{workspace, (int64_t)need, 1};
+    const Span z{Z_shards, g.M * g.N, elem_size(z_dtype)}, dy{dY_shards, g.M * g.N, elem_size(dy_dtype)}, dz{dZ_shards, g.M * g.N, elem_size(dz_dtype)};
+    const Span db{dbias_diag, g.q * g.N, 4}, ws{workspace, (int64_t)need, 1};
     if (overlap(dz, z) || overlaps_but_in_place(dz, dy) || overlap(db, dz) || overlaps_any(ws, {z, dy, dz, db})) return CUBE3D_EINVAL;
     return epilogue_bwd(g, kind, z_dtype, dy_dtype, dz_dtype, Z_shards, dY_shards, dZ_shards, static_cast<float *>(dbias_diag),
                         static_cast<float *>(workspace), static_cast<hipStream_t>(stream));
